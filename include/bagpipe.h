@@ -12,6 +12,11 @@
  *   bp_embbag_fwd         EmbeddingBag-sum forward over cache slots (Section 2.1, embedding lookup)
  *   bp_embbag_bwd_update  deterministic backward + fused sparse optimizer step on cached rows
  *
+ * For models that read sequences of cached rows, beside them:
+ *   bp_relpos_bias_fwd / _bwd, bp_relpos_update   a learned bias by distance, its gradient and its step
+ *   bp_embbag_attn_fwd / _bwd                     bags pooled by attention instead of a sum, and the gradients
+ *   bp_evict_by_weight                            lists over their budget lose the entries attended to least
+ *
  * Conventions
  *   - Every function returns BP_OK (0) or a negative bp_status.  bp_last_error_message() gives detail
  *     for the calling thread's last failure.
@@ -442,6 +447,147 @@ int bp_embbag_bwd_update_grouped_static(const bp_config* cfg, void* cache_w, voi
                                         const int32_t* grouped_lookups, const bp_row_rec* row_recs, int64_t n_rows,
                                         const bp_piece_rec* piece_recs, int64_t n_pieces, const int64_t* bag_offsets,
                                         int64_t n_lookups, int64_t bags, const float* grad_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (5) Bias by distance: a learned table with one row per bucket of distances and one column per head, looked up for every
+ * pair of a query and a key.  distance = query position - key position; bucket(n) = number of borders <= n for n = |distance|.
+ * ------------------------------------------------------------------------------------------------ */
+#define BP_RELPOS_MAX_BUCKETS 64
+typedef struct bp_relpos {
+    int32_t buckets;        /* of one direction, 1 .. BP_RELPOS_MAX_BUCKETS */
+    int32_t two_sided;      /* 0: keys after the query (distance < 0) are not seen.  1: they have buckets of their own, table
+                               rows buckets + bucket(n) */
+    const int32_t* borders; /* host [buckets - 1], ascending, 1 <= border < 2^30: the smallest distance of buckets 1, 2, ...
+                               (NULL when buckets == 1) */
+} bp_relpos;                /* the table has buckets * (two_sided ? 2 : 1) rows */
+
+/* Borders in common use (host, [buckets - 1]): with e = max(1, buckets / 2) the buckets 0 .. e - 1 hold one distance each, the
+ * borders behind them are the smallest whole numbers >= e * (far / e)^(t / (buckets - e)), t = 0, 1, ..., each at least one
+ * more than the one before; distances from about `far` on share the last bucket.  Computed in whole numbers.
+ * 1 <= buckets <= BP_RELPOS_MAX_BUCKETS, 1 <= far < 2^24 (a value below e + 1 counts as e + 1). */
+int bp_relpos_borders(int32_t buckets, int32_t far, int32_t* borders);
+
+/*
+ * out[h, i, j] = table[row of the distance (q_start + i) - j][h]; -infinity where the key is not seen.
+ * table       device, fp32 [rows][heads]
+ * out         device, out_dtype (BP_F32, or BP_BF16 rounded to nearest even) [heads][lq][lk]; row_stride and head_stride are
+ *             the elements from one (h, i) to the next i and the next h; 0 = dense; else row_stride >= lk and
+ *             head_stride >= (lq - 1) * row_stride + lk.  What lies between the rows is left as it is.
+ * q_start     position of query 0 (lq = 1 and q_start = keys so far - 1: the form for a single token), |q_start| < 2^30
+ * Limits: heads <= 65,535; lq, lk < 2^30, heads * lq * lk < 2^40.  Nothing is written when one of them is 0.
+ * `out` is aligned to its element.  Asynchronous on `stream`.
+ */
+int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_t heads, int64_t lq, int64_t lk, int64_t q_start, void* out,
+                       int32_t out_dtype, int64_t row_stride, int64_t head_stride, void* stream);
+
+/*
+ * grad_table[r, h] = sum of grad_out[b, h, i, j] over all b, i, j whose distance has table row r: the bias is broadcast over a
+ * batch, so its gradients add up over it.  Deterministic: fp32 sums of short runs of pairs, fp64 from there on, rounded once,
+ * in an order that the sizes and strides fix.  Pairs that are not seen are left out, whatever grad_out holds there.
+ * grad_out    device, grad_dtype [batch][heads][lq][lk] with strides as for `out` above (batch_stride likewise, 0 = dense)
+ * grad_table  device, fp32 [rows][heads], written whole (rows without a pair get 0)
+ * workspace   device, bp_relpos_bias_bwd_workspace_bytes() bytes, 256-byte aligned
+ * Limits as above, with batch * heads * lq * lk < 2^40 and batch <= 65,535.  Asynchronous on `stream`.
+ */
+int bp_relpos_bias_bwd_workspace_bytes(const bp_relpos* rp, int64_t batch, int32_t heads, int64_t lq, int64_t lk, size_t* bytes);
+int bp_relpos_bias_bwd(const bp_relpos* rp, const void* grad_out, int32_t grad_dtype, int64_t batch, int32_t heads, int64_t lq,
+                       int64_t lk, int64_t row_stride, int64_t head_stride, int64_t batch_stride, int64_t q_start, float* grad_table,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One step on the table by the rule, learning rate and epsilon of cfg (the three rules of (4); a row of the row-wise rule is a
+ * bucket, its mean of squares is taken over the heads).  cfg's row sizes and strides are not looked at.
+ * table   device, fp32 [rows][heads], updated in place;  state  device, fp32 [rows][heads] (BP_ADAGRAD), [rows]
+ * (BP_ADAGRAD_ROWWISE) or NULL (BP_SGD).  Asynchronous on `stream`.
+ */
+int bp_relpos_update(const bp_config* cfg, const bp_relpos* rp, int32_t heads, float* table, float* state, const float* grad_table,
+                     void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (6) Bags pooled by attention: as (3), with weights that a query of the bag's own gives its rows.  A row holds a key, and a
+ * value, for each of kv_heads heads; query head h reads kv head h / (q_heads / kv_heads).  For query head h of bag b and entry k:
+ *     c = scale * <q[b,h], key>;  cap > 0: c = cap * tanh(c / cap);  rp given: c += bias_table[row of q_pos[b] - lookup_pos[k]][h]
+ *     p = softmax of c over the bag's entries that are seen;  out[b,h] = sum p * value;  lse[b,h] = log sum exp(c)
+ * An entry is seen when its slot lies in [0, capacity) and rp, if given, sees its distance.  A bag that sees nothing has
+ * out = 0 and lse = -infinity; an entry that is not seen has no part in anything, whatever its row holds.
+ * With lists of one sequence's cached tokens as bags this is the attention of one new token per sequence over its cache.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct bp_attn {
+    int32_t q_heads;      /* a multiple of kv_heads, at most 16 times as many */
+    int32_t kv_heads;     /* 1 .. 64 */
+    int32_t head_dim;     /* d: a multiple of 8, 8 .. 256 */
+    int32_t value_offset; /* keys are elements [0, kv_heads * d) of a row, values begin here: 0 (the keys are the values too), or
+                             a multiple of 8 that is at least kv_heads * d.  cfg->dim holds both; what else a row holds is not
+                             read */
+    float scale;
+    float cap;            /* 0: none */
+} bp_attn;
+
+/*
+ * cache_w      device, as for bp_embbag_fwd (strided rows too); storage fp32 or bf16, arithmetic fp32
+ * lookup_slots device, int32 [n_lookups]
+ * bag_offsets  device, int64 [bags + 1] from 0 to n_lookups, ascending: bag b's stretch is [bag_offsets[b], bag_offsets[b+1])
+ * bag_lengths  device, int32 [bags], or NULL: of its stretch a bag uses the first bag_lengths[b] entries only (lists that grow
+ *              in place); values outside [0, stretch] are brought into it
+ * q            device, fp32 [bags][q_heads][d]
+ * rp, q_pos, lookup_pos, bias_table: all NULL, or all given: int32 [bags], int32 [n_lookups], fp32 [rows][q_heads] (device)
+ * out, lse     device, fp32 [bags][q_heads][d], fp32 [bags][q_heads]
+ * weight_in, weight_out  device, fp32 [n_lookups]; weight_out may be NULL, else weight_out[k] = weight_in[k] + sum over the query
+ *              heads of p, for every entry that a bag uses (the others keep what weight_out holds).  weight_in may be NULL (zeros),
+ *              or weight_out itself.
+ * workspace    device, bp_embbag_attn_fwd_workspace_bytes() bytes, 256-byte aligned (calls that overlap in time need their own)
+ * q, out, cache_w, bias_table: 16-byte aligned.  Softmax and sums are fp32; an order that sizes fix.  Asynchronous on `stream`.
+ */
+int bp_embbag_attn_fwd_workspace_bytes(const bp_config* cfg, const bp_attn* at, int64_t n_lookups, int64_t bags, int32_t with_weights,
+                                       size_t* bytes);
+int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const bp_relpos* rp, const void* cache_w, const int32_t* lookup_slots,
+                       const int64_t* bag_offsets, const int32_t* bag_lengths, int64_t n_lookups, int64_t bags, const float* q,
+                       const int32_t* q_pos, const int32_t* lookup_pos, const float* bias_table, float* out, float* lse,
+                       const float* weight_in, float* weight_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of (6), from its inputs, its out and lse, and grad_out (device, fp32 [bags][q_heads][d]):
+ * grad_q      device, fp32 [bags][q_heads][d]
+ * grad_rows   device, fp32 [n_lookups][dim]: the gradient of every used entry's row (zeros for entries that are not seen and for
+ *             elements that are neither key nor value; entries that no bag uses keep what it holds).  It is what
+ *             bp_embbag_bwd_update[_grouped] takes as grad_out with one lookup per bag: rows looked up several times are
+ *             coalesced and stepped there.
+ * grad_bias   device, fp32 [rows][q_heads], written whole, when rp is given (else NULL)
+ * Deterministic: the same inputs give the same bits.  Other arguments as above; workspace:
+ * bp_embbag_attn_bwd_workspace_bytes().  Asynchronous on `stream`.
+ */
+int bp_embbag_attn_bwd_workspace_bytes(const bp_config* cfg, const bp_attn* at, const bp_relpos* rp, int64_t n_lookups, int64_t bags,
+                                       size_t* bytes);
+int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const bp_relpos* rp, const void* cache_w, const int32_t* lookup_slots,
+                       const int64_t* bag_offsets, const int32_t* bag_lengths, int64_t n_lookups, int64_t bags, const float* q,
+                       const int32_t* q_pos, const int32_t* lookup_pos, const float* bias_table, const float* out, const float* lse,
+                       const float* grad_out, float* grad_q, float* grad_rows, float* grad_bias, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (7) Eviction by accumulated weight: a list (bag) of more than `budget` entries loses its length - budget entries of the lowest
+ * weight.  Its first `sinks` and its last `recent` entries never leave; of equal weights the earlier entry leaves first (-0
+ * equals 0, NaN counts as above every number).  The others keep their order.
+ *
+ * bag_offsets, bag_lengths   device, as in (6) (bag_lengths may be NULL)
+ * weight, ids, slots, pos    device, [n] fp32, int64, int32, int32; ids and pos may be NULL
+ * kept_weight, kept_ids, kept_slots, kept_pos   device, [n]: bag b's remaining entries from bag_offsets[b] on; what lies behind
+ *             them is left as it is.  They must not overlap the input arrays (entries move); NULL where the input is NULL (kept_weight may be NULL
+ *             always).  The caller swaps the two sets.
+ * kept_lengths               device, int32 [bags]: min(length, budget).  Not bag_lengths itself.
+ * evict_ids, evict_slots     device, int64 and int32 [list_capacity]: what left, bag by bag, each in list order; entries behind
+ *             the last one are -1, so that bp_cache_apply, which skips those, takes the lists at their capacity without the host
+ *             knowing the count.  evict_ids NULL when ids is.  Entries beyond list_capacity are not listed.
+ * evict_offsets              device, int64 [bags + 1]: CSR offsets of the bags into the evict lists
+ * budget >= 1, sinks, recent >= 0, sinks + recent <= budget; n < 2^31, bags < 2^24.
+ * workspace   device, bp_evict_by_weight_workspace_bytes() bytes, 256-byte aligned.  Asynchronous on `stream`.
+ * ------------------------------------------------------------------------------------------------ */
+int bp_evict_by_weight_workspace_bytes(int64_t n, int64_t bags, size_t* bytes);
+int bp_evict_by_weight(const int64_t* bag_offsets, const int32_t* bag_lengths, int64_t n, int64_t bags, int32_t budget, int32_t sinks,
+                       int32_t recent, const float* weight, const int64_t* ids, const int32_t* slots, const int32_t* pos,
+                       float* kept_weight, int64_t* kept_ids, int32_t* kept_slots, int32_t* kept_pos, int32_t* kept_lengths,
+                       int64_t* evict_ids, int32_t* evict_slots, int64_t list_capacity, int64_t* evict_offsets, void* workspace,
+                       size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Diagnostics.

@@ -19,6 +19,9 @@ from .binding import (  # noqa: F401
     bp_embbag_bwd_ticket_bytes, bwd_tickets, piece_capacity,
     bp_embbag_bwd_update_grouped_static, bp_embbag_bwd_update_grouped_static_bytes,
     bp_embbag_bwd_update_grouped_static_max_bytes,
+    bp_relpos, bp_attn, make_relpos, make_attn, relpos_rows, bp_relpos_borders, bp_relpos_bias_fwd, bp_relpos_bias_bwd,
+    bp_relpos_bias_bwd_workspace_bytes, bp_relpos_update, bp_embbag_attn_fwd, bp_embbag_attn_fwd_workspace_bytes,
+    bp_embbag_attn_bwd, bp_embbag_attn_bwd_workspace_bytes, bp_evict_by_weight, bp_evict_by_weight_workspace_bytes,
     bp_error_string, bp_last_error_message, bp_version,
     bp_copy_calibration, bp_gather_calibration, bp_scatter_calibration, bp_profile_enable, bp_profile_select, bp_profile_bracket_overhead, bp_profile_collect, bp_profile_get, profile_totals, profile_spread,
 )

@@ -31,6 +31,15 @@ class bp_config(ctypes.Structure):
                 ("cache_w_stride", ctypes.c_int64), ("cache_state_stride", ctypes.c_int64)]
 
 
+class bp_relpos(ctypes.Structure):
+    _fields_ = [("buckets", ctypes.c_int32), ("two_sided", ctypes.c_int32), ("borders", ctypes.c_void_p)]
+
+
+class bp_attn(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("value_offset", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float)]
+
+
 class _bp_plan_state(ctypes.Structure):
     _fields_ = [("n_resident", ctypes.c_int64), ("resident_ids", ctypes.c_void_p), ("ring", ctypes.c_void_p)]
 
@@ -120,6 +129,24 @@ def load_library():
     lib.bp_profile_bracket_overhead.restype = ctypes.c_int
     lib.bp_profile_select.argtypes = [ctypes.c_uint64]
     lib.bp_profile_select.restype = ctypes.c_int
+    rpp, atp = ctypes.POINTER(bp_relpos), ctypes.POINTER(bp_attn)
+    szp = ctypes.POINTER(sz)
+    lib.bp_relpos_borders.argtypes = [i32, i32, vp]
+    lib.bp_relpos_bias_fwd.argtypes = [rpp, vp, i32, i64, i64, i64, vp, i32, i64, i64, vp]
+    lib.bp_relpos_bias_bwd_workspace_bytes.argtypes = [rpp, i64, i32, i64, i64, szp]
+    lib.bp_relpos_bias_bwd.argtypes = [rpp, vp, i32, i64, i32, i64, i64, i64, i64, i64, i64, vp, vp, sz, vp]
+    lib.bp_relpos_update.argtypes = [cfgp, rpp, i32, vp, vp, vp, vp]
+    lib.bp_embbag_attn_fwd_workspace_bytes.argtypes = [cfgp, atp, i64, i64, i32, szp]
+    lib.bp_embbag_attn_fwd.argtypes = [cfgp, atp, rpp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bp_embbag_attn_bwd_workspace_bytes.argtypes = [cfgp, atp, rpp, i64, i64, szp]
+    lib.bp_embbag_attn_bwd.argtypes = [cfgp, atp, rpp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bp_evict_by_weight_workspace_bytes.argtypes = [i64, i64, szp]
+    lib.bp_evict_by_weight.argtypes = [vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+    for name in ("bp_relpos_borders", "bp_relpos_bias_fwd", "bp_relpos_bias_bwd_workspace_bytes", "bp_relpos_bias_bwd",
+                 "bp_relpos_update", "bp_embbag_attn_fwd_workspace_bytes", "bp_embbag_attn_fwd",
+                 "bp_embbag_attn_bwd_workspace_bytes", "bp_embbag_attn_bwd", "bp_evict_by_weight_workspace_bytes",
+                 "bp_evict_by_weight"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("bp_oracle_plan_workspace_bytes", "bp_oracle_plan", "bp_cache_apply", "bp_embbag_fwd",
                  "bp_embbag_bwd_update_workspace_bytes", "bp_embbag_bwd_update", "bp_version",
                  "bp_embbag_bwd_update_grouped_workspace_bytes", "bp_embbag_bwd_update_grouped",
@@ -637,6 +664,170 @@ def bp_embbag_bwd_update_grouped_static(cfg: bp_config, cache_w, cache_state, gr
         ctypes.byref(cfg), _ptr(cache_w), _ptr(cache_state), _ptr(grouped_lookups), _ptr(row_recs),
         _needed_rows(row_recs), _ptr(piece_recs) if n_pieces else None, n_pieces,
         _ptr(bag_offsets), n, int(bags), _ptr(grad_out), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------
+# (5) bias by distance
+# ---------------------------------------------------------------------------------------------------
+def _needs(t, dtype: str, n: int, name: str) -> Optional[int]:
+    """Address of a contiguous array of n elements of `dtype`; a call that would read or write past it raises here."""
+    if type(t) is _Span:
+        if t.n < n:
+            raise ValueError(f"{name}: {t.n} elements, {n} needed")
+        return t.ptr
+    if not t.is_contiguous() or str(t.dtype) != "torch." + dtype or t.numel() < n:
+        raise ValueError(f"{name}: contiguous {dtype} with {n} elements needed, not {str(t.dtype)[6:]} {tuple(t.shape)}")
+    return t.data_ptr() or None
+
+
+def _optional(t, dtype: str, n: int, name: str) -> Optional[int]:
+    return None if t is None else _needs(t, dtype, n, name)
+
+
+def make_relpos(borders, two_sided: bool = False) -> bp_relpos:
+    """borders: the smallest distance of buckets 1, 2, ... (bp_relpos_borders makes those in common use)."""
+    b = np.ascontiguousarray(borders, dtype=np.int32)
+    rp = bp_relpos(b.shape[0] + 1, int(bool(two_sided)), b.ctypes.data if b.shape[0] else None)
+    rp.kept = b          # the struct holds an address
+    return rp
+
+
+def relpos_rows(rp: bp_relpos) -> int:
+    return rp.buckets * (2 if rp.two_sided else 1)
+
+
+def bp_relpos_borders(buckets: int, far: int) -> np.ndarray:
+    out = np.zeros(max(int(buckets) - 1, 0), dtype=np.int32)
+    _check(load_library().bp_relpos_borders(int(buckets), int(far), out.ctypes.data if out.shape[0] else None))
+    return out
+
+
+def _grid(t, dims: int, name: str):
+    """Dtype code and strides (0 where a size of one leaves them open) of an array whose last dimension is dense."""
+    if t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: {dims} dimensions needed, the last one dense")
+    code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(t.dtype))
+    if code is None:
+        raise ValueError(f"{name}: float32 or bfloat16 needed, not {t.dtype}")
+    return code, [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims - 1)]
+
+
+def bp_relpos_bias_fwd(rp: bp_relpos, table, q_start: int, out, stream=None) -> None:
+    """table: fp32 [rows, heads]; out: fp32 or bf16 [heads, lq, lk], written in place (rows and heads may be strided)."""
+    heads, lq, lk = out.shape
+    code, (hs, rs) = _grid(out, 3, "out")
+    tp = _needs(table, "float32", relpos_rows(rp) * heads, "table")
+    _check(load_library().bp_relpos_bias_fwd(ctypes.byref(rp), tp, heads, lq, lk, int(q_start), out.data_ptr() or None, code,
+                                             rs, hs, _stream(stream)))
+
+
+def bp_relpos_bias_bwd_workspace_bytes(rp: bp_relpos, batch: int, heads: int, lq: int, lk: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().bp_relpos_bias_bwd_workspace_bytes(ctypes.byref(rp), int(batch), int(heads), int(lq), int(lk),
+                                                             ctypes.byref(out)))
+    return int(out.value)
+
+
+def bp_relpos_bias_bwd(rp: bp_relpos, grad_out, q_start: int, grad_table, workspace, stream=None) -> None:
+    """grad_out: fp32 or bf16 [batch, heads, lq, lk] (strided but for the last dimension); grad_table: fp32 [rows, heads]."""
+    batch, heads, lq, lk = grad_out.shape
+    code, (bs, hs, rs) = _grid(grad_out, 4, "grad_out")
+    tp = _needs(grad_table, "float32", relpos_rows(rp) * heads, "grad_table")
+    _check(load_library().bp_relpos_bias_bwd(ctypes.byref(rp), grad_out.data_ptr() or None, code, batch, heads, lq, lk, rs, hs, bs,
+                                             int(q_start), tp, _ptr(workspace), _count(workspace), _stream(stream)))
+
+
+def bp_relpos_update(cfg: bp_config, rp: bp_relpos, table, state, grad_table, stream=None) -> None:
+    """One step on the table by cfg's optimizer, learning rate and epsilon.  table, grad_table: fp32 [rows, heads]."""
+    rows, heads = relpos_rows(rp), int(table.shape[1])
+    n_state = {SGD: 0, ADAGRAD: rows * heads}.get(cfg.optimizer, rows)
+    _check(load_library().bp_relpos_update(ctypes.byref(cfg), ctypes.byref(rp), heads, _needs(table, "float32", rows * heads, "table"),
+                                           _optional(state, "float32", n_state, "state"),
+                                           _needs(grad_table, "float32", rows * heads, "grad_table"), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------
+# (6) bags pooled by attention
+# ---------------------------------------------------------------------------------------------------
+def make_attn(q_heads: int, kv_heads: int, head_dim: int, value_offset: Optional[int] = None, scale: Optional[float] = None,
+              cap: float = 0.0) -> bp_attn:
+    """value_offset: None = values right behind the keys, 0 = the keys are the values; scale: None = head_dim ** -0.5."""
+    return bp_attn(int(q_heads), int(kv_heads), int(head_dim), int(kv_heads) * int(head_dim) if value_offset is None else int(value_offset),
+                   float(head_dim) ** -0.5 if scale is None else float(scale), float(cap))
+
+
+def bp_embbag_attn_fwd_workspace_bytes(cfg: bp_config, at: bp_attn, n_lookups: int, bags: int, with_weights: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().bp_embbag_attn_fwd_workspace_bytes(ctypes.byref(cfg), ctypes.byref(at), int(n_lookups), int(bags),
+                                                             int(bool(with_weights)), ctypes.byref(out)))
+    return int(out.value)
+
+
+def _attn_inputs(cfg, at, rp, cache_w, lookup_slots, bag_offsets, bag_lengths, bags, q, q_pos, lookup_pos, bias_table):
+    n, bags = _needed_count(lookup_slots), int(bags)
+    rows = bags * at.q_heads * at.head_dim
+    return n, rows, (ctypes.byref(cfg), ctypes.byref(at), None if rp is None else ctypes.byref(rp), _ptr(cache_w),
+                     _needs(lookup_slots, "int32", n, "lookup_slots"), _needs(bag_offsets, "int64", bags + 1, "bag_offsets"),
+                     _optional(bag_lengths, "int32", bags, "bag_lengths"), n, bags, _needs(q, "float32", rows, "q"),
+                     _optional(q_pos, "int32", bags, "q_pos"), _optional(lookup_pos, "int32", n, "lookup_pos"),
+                     _optional(bias_table, "float32", 0 if rp is None else relpos_rows(rp) * at.q_heads, "bias_table"))
+
+
+def bp_embbag_attn_fwd(cfg: bp_config, at: bp_attn, cache_w, lookup_slots, bag_offsets, bags: int, q, out, lse, workspace,
+                       bag_lengths=None, relpos: Optional[bp_relpos] = None, q_pos=None, lookup_pos=None, bias_table=None,
+                       weight_in=None, weight_out=None, stream=None) -> None:
+    """q, out: fp32 [bags, q_heads, head_dim]; lse: fp32 [bags, q_heads]; weights: fp32, one per lookup.  relpos, q_pos,
+    lookup_pos and bias_table go together."""
+    n, rows, given = _attn_inputs(cfg, at, relpos, cache_w, lookup_slots, bag_offsets, bag_lengths, bags, q, q_pos, lookup_pos, bias_table)
+    _check(load_library().bp_embbag_attn_fwd(
+        *given, _needs(out, "float32", rows, "out"), _needs(lse, "float32", int(bags) * at.q_heads, "lse"),
+        _optional(weight_in, "float32", n, "weight_in"), _optional(weight_out, "float32", n, "weight_out"), _ptr(workspace),
+        _count(workspace), _stream(stream)))
+
+
+def bp_embbag_attn_bwd_workspace_bytes(cfg: bp_config, at: bp_attn, relpos: Optional[bp_relpos], n_lookups: int, bags: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().bp_embbag_attn_bwd_workspace_bytes(ctypes.byref(cfg), ctypes.byref(at),
+                                                             None if relpos is None else ctypes.byref(relpos), int(n_lookups),
+                                                             int(bags), ctypes.byref(out)))
+    return int(out.value)
+
+
+def bp_embbag_attn_bwd(cfg: bp_config, at: bp_attn, cache_w, lookup_slots, bag_offsets, bags: int, q, out, lse, grad_out, grad_q,
+                       grad_rows, grad_bias, workspace, bag_lengths=None, relpos: Optional[bp_relpos] = None, q_pos=None,
+                       lookup_pos=None, bias_table=None, stream=None) -> None:
+    """grad_q as q; grad_rows: fp32 [n_lookups, dim]; grad_bias: fp32 as bias_table, with relpos, else None."""
+    n, rows, given = _attn_inputs(cfg, at, relpos, cache_w, lookup_slots, bag_offsets, bag_lengths, bags, q, q_pos, lookup_pos, bias_table)
+    _check(load_library().bp_embbag_attn_bwd(
+        *given, _needs(out, "float32", rows, "out"), _needs(lse, "float32", int(bags) * at.q_heads, "lse"),
+        _needs(grad_out, "float32", rows, "grad_out"), _needs(grad_q, "float32", rows, "grad_q"),
+        _needs(grad_rows, "float32", n * cfg.dim, "grad_rows"),
+        _optional(grad_bias, "float32", 0 if relpos is None else relpos_rows(relpos) * at.q_heads, "grad_bias"), _ptr(workspace),
+        _count(workspace), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------
+# (7) eviction by accumulated weight
+# ---------------------------------------------------------------------------------------------------
+def bp_evict_by_weight_workspace_bytes(n: int, bags: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().bp_evict_by_weight_workspace_bytes(int(n), int(bags), ctypes.byref(out)))
+    return int(out.value)
+
+
+def bp_evict_by_weight(bag_offsets, bag_lengths, bags: int, budget: int, sinks: int, recent: int, weight, ids, slots, pos, kept_ids,
+                       kept_slots, kept_pos, kept_weight, kept_lengths, evict_ids, evict_slots, evict_offsets, workspace,
+                       stream=None) -> None:
+    """ids, pos and kept_weight (with kept_ids, kept_pos, evict_ids) may be None.  The evict lists' capacity is evict_slots'."""
+    n, bags, cap = _needed_count(slots), int(bags), _count(evict_slots)
+    _check(load_library().bp_evict_by_weight(
+        _needs(bag_offsets, "int64", bags + 1, "bag_offsets"), _optional(bag_lengths, "int32", bags, "bag_lengths"), n, bags, int(budget),
+        int(sinks), int(recent), _needs(weight, "float32", n, "weight"), _optional(ids, "int64", n, "ids"),
+        _needs(slots, "int32", n, "slots"), _optional(pos, "int32", n, "pos"), _optional(kept_weight, "float32", n, "kept_weight"),
+        _optional(kept_ids, "int64", n, "kept_ids"), _needs(kept_slots, "int32", n, "kept_slots"), _optional(kept_pos, "int32", n, "kept_pos"),
+        _needs(kept_lengths, "int32", bags, "kept_lengths"), _optional(evict_ids, "int64", cap, "evict_ids"),
+        _optional(evict_slots, "int32", cap, "evict_slots"), cap, _needs(evict_offsets, "int64", bags + 1, "evict_offsets"), _ptr(workspace),
+        _count(workspace), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------------------------

@@ -121,6 +121,14 @@ enum KernelId {
     K_BWD_REDUCE_UPDATE,
     K_FILL,
     K_COPY,
+    K_RELPOS_FWD,
+    K_RELPOS_BWD,
+    K_RELPOS_JOIN,
+    K_RELPOS_UPDATE,
+    K_ATTN_FWD,
+    K_ATTN_BWD,
+    K_ATTN_JOIN,
+    K_EVICT_SELECT,
     K_NUM_KERNELS
 };
 

@@ -25,7 +25,9 @@ the prefetches of batch i, so a row is never fetched while an update to it is st
 With a whole-trace plan whose L_eff >= 2, maintain() uses bp_cache_apply_handoff (one launch, no staging: the rows
 that leave and the rows that enter a slot go through the same lane group; handoff=True, default); otherwise, with
 duplex=True (default) and L_eff >= 2, bp_cache_apply_duplex (staging area, then writes to and reads from the backing
-table in one launch); otherwise bp_cache_apply.  With grouping=True (default) the plan also lists every batch's lookups grouped by row and the backward pass
+table in one launch); otherwise bp_cache_apply.
+Bags pooled by attention instead of a sum (needs the slot map): attend() / attend_backward_update() in the place of forward() /
+backward_update().  With grouping=True (default) the plan also lists every batch's lookups grouped by row and the backward pass
 uses bp_embbag_bwd_update_grouped (no sort at run time); with grouping=False it sorts the slots itself.
 """
 from __future__ import annotations
@@ -88,6 +90,7 @@ class CachedEmbeddingTrainer:
         self._bwd_ws = None
         self._tickets = None           # counters of the backward pass: zeroed here once, every call leaves them zero
         self._out = None
+        self._attn_ws = self._grad_rows = None      # attention over bags: workspace, gradient of every lookup's row
         self._pipeline = None
         self._plan_state = None        # chunked planning: state of the cache at the last chunk boundary
         self._carried_evict = None     # evictions of the previous chunk's last batch, applied before this chunk's first
@@ -265,3 +268,43 @@ class CachedEmbeddingTrainer:
         else:
             B.bp_embbag_bwd_update(self.cfg, self._cw, self._cs, B._span(p.lookup_slots, a, b), bag_offsets_dev,
                                    bags, grad_out, self._bwd_ws, self._tickets, stream=stream)
+
+    # ---- (6) bags pooled by attention
+    def _attn_workspace(self, need: int):
+        if self._attn_ws is None or self._attn_ws.numel() < need:
+            import torch
+            self._attn_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._attn_ws
+
+    def attend(self, i: int, at: B.bp_attn, bag_offsets_dev, bags: int, q, out=None, lse=None, stream=None, **given):
+        """Pools batch i's bags by attention (bp_embbag_attn_fwd); given: its optional arguments (bag_lengths, relpos, ...).
+        Returns out [bags, q_heads, head_dim] and lse [bags, q_heads]."""
+        import torch
+        n = self.iter_offsets.item(i + 1) - self.iter_offsets.item(i)
+        if self.plan_.lookup_slots is None:
+            raise ValueError("attention over bags needs a slot per lookup; plan with slot_map=True")
+        out = torch.empty_like(q) if out is None else out
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if lse is None else lse
+        ws = self._attn_workspace(B.bp_embbag_attn_fwd_workspace_bytes(self.cfg, at, n, bags, given.get("weight_out") is not None))
+        B.bp_embbag_attn_fwd(self.cfg, at, self._cw, self.slots(i), bag_offsets_dev, bags, q, out, lse, ws, stream=stream, **given)
+        return out, lse
+
+    def attend_backward_update(self, i: int, at: B.bp_attn, bag_offsets_dev, bags: int, q, out, lse, grad_out, grad_q=None,
+                               grad_bias=None, stream=None, grouped: Optional[bool] = None, **given):
+        """Gradients of attend() (bp_embbag_attn_bwd); the rows' ones go on into backward_update, a bag for every lookup, which
+        steps the rows.  Returns the gradients of q and, with relpos, of the bias table (bp_relpos_update steps that)."""
+        import torch
+        n, rp = self.iter_offsets.item(i + 1) - self.iter_offsets.item(i), given.get("relpos")
+        grad_q = torch.empty_like(q) if grad_q is None else grad_q
+        if rp is not None and grad_bias is None:
+            grad_bias = torch.empty_like(given["bias_table"])
+        if self._grad_rows is None or self._grad_rows.shape[0] < n:
+            self._grad_rows = torch.zeros((n, int(self.cfg.dim)), dtype=torch.float32, device=self.device)
+        elif given.get("bag_lengths") is not None:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) and stream else stream):
+                self._grad_rows[:n].zero_()                  # lookups that no bag uses have no gradient
+        ws = self._attn_workspace(B.bp_embbag_attn_bwd_workspace_bytes(self.cfg, at, rp, n, bags))
+        B.bp_embbag_attn_bwd(self.cfg, at, self._cw, self.slots(i), bag_offsets_dev, bags, q, out, lse, grad_out, grad_q,
+                             self._grad_rows[:n], grad_bias, ws, stream=stream, **given)
+        self.backward_update(i, None, n, self._grad_rows[:n], stream=stream, grouped=grouped)
+        return grad_q, grad_bias
