@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbagpipe_hip.so")
 SOURCES = ["abi.hip", "planner.hip", "cache_apply.hip", "pipeline.hip", "embbag_fwd.hip", "embbag_bwd.hip",
-           "relpos_bias.hip", "embbag_attn.hip", "evict.hip"]
+           "relpos_bias.hip", "embbag_attn_fwd.hip", "embbag_attn_bwd.hip", "evict.hip"]
 
 # -ffp-contract=off: every fp32 operation rounds once (no fused multiply-add), which keeps the update
 #   arithmetic reproducible and close to the fp64 reference.
