@@ -56,64 +56,219 @@ bool at_least(const Whole& a, const Whole& b) {
 
 constexpr int64_t kBiasMost = int64_t(1) << 40;
 
-// One element a thread.
+// A workgroup writes a stretch of keys for up to kBiasRows queries of one head.  What it writes depends on j - i alone, so the
+// looked-up values lie in LDS as one line, of which every query takes a stretch, shifted by one from the query before.  16
+// bytes a store, aligned in memory (the first and last of a row's chunks may be cut), whatever a row's own alignment.  bf16 lines
+// are kept as pairs, once from every even and once from every odd element on.  Bound by the stores.
+constexpr int kBiasBlock = 256, kBiasRows = 32, kBiasChunks = 256;
 template <typename T>
-__global__ __launch_bounds__(256) void relpos_bias_fwd_kernel(Relpos rp, const float* __restrict__ table, int heads, int64_t lq,
-                                                              int64_t lk, int64_t q_start, T* __restrict__ out, int64_t row_stride,
-                                                              int64_t head_stride) {
+__global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, const float* __restrict__ table, int heads, int64_t lq,
+                                                                     int64_t lk, int64_t q_start, T* __restrict__ out, int64_t row_stride,
+                                                                     int64_t head_stride, int chunks, int64_t tiles) {
+    constexpr int PER = 16 / sizeof(T), MOST = kBiasChunks * PER + 2 * PER + kBiasRows + 8;
     __shared__ int32_t borders[BP_RELPOS_MAX_BUCKETS];
+    __shared__ float column[2 * BP_RELPOS_MAX_BUCKETS];
+    __shared__ uint32_t line[MOST];                       // fp32: a value a word; bf16: words 0 .. MOST/2 even pairs, then odd ones
+    const int64_t j0 = (int64_t)(blockIdx.x % tiles) * chunks * PER, i0 = (int64_t)(blockIdx.x / tiles) * kBiasRows;
+    const int h = blockIdx.y, rows = (int)min((int64_t)kBiasRows, lq - i0);
     if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = rp.borders[threadIdx.x];
+    for (int r = threadIdx.x; r < rp.rows(); r += kBiasBlock) column[r] = table[(int64_t)r * heads + h];
     __syncthreads();
-    const int64_t n = heads * lq * lk;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
-        const int64_t j = e % lk, i = e / lk % lq, h = e / lk / lq;
-        const int row = relpos_row(q_start + i - j, borders, rp.buckets, rp.two_sided);
-        const float v = row < 0 ? -INFINITY : table[(int64_t)row * heads + h];
-        T* const to = out + h * head_stride + i * row_stride + j;
-        if constexpr (sizeof(T) == 2) *to = (T)f32_to_bf16_bits(v);
-        else *to = v;
-    }
-}
-
-// A bucket's pairs lie in a stretch of a query's keys, so a wavefront adds a query's stretches one by one.
-constexpr int kGradRows = 16;          // queries of one (batch, head) a wavefront takes
-template <typename T>
-__global__ __launch_bounds__(64) void relpos_bias_bwd_kernel(Relpos rp, const T* __restrict__ grad, int64_t lq, int64_t lk,
-                                                             int64_t row_stride, int64_t head_stride, int64_t batch_stride,
-                                                             int64_t q_start, double* __restrict__ partial) {
-    const int lane = threadIdx.x, rows = rp.rows();
-    const T* const g = grad + blockIdx.z * batch_stride + blockIdx.y * head_stride;
-    const int64_t part = ((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
-    for (int r = 0; r < rows; ++r) {
-        const bool later = r >= rp.buckets;
-        const int b = later ? r - rp.buckets : r;
-        const int64_t near = b ? rp.borders[b - 1] : later ? 1 : 0, far = b + 1 < rp.buckets ? rp.borders[b] : int64_t(1) << 40;
-        double sum = 0;
-        for (int64_t i = (int64_t)blockIdx.x * kGradRows; i < min(lq, ((int64_t)blockIdx.x + 1) * kGradRows); ++i) {
-            const int64_t q = q_start + i;
-            const int64_t first = max(int64_t(0), later ? q + near : q - far + 1), end = min(lk, later ? q + far : q - near + 1);
-            float run = 0.f;
-            for (int64_t j = first + lane; j < end; j += 64) {
-                if constexpr (sizeof(T) == 2) run += bf16_bits_to_f32(g[i * row_stride + j]);
-                else run += g[i * row_stride + j];
-            }
-            sum += run;
+    // line[x] is the value of key j for query i with x = (j - j0 + PER) + (rows - 1 - (i - i0)): a cut chunk begins up to PER - 1
+    // keys before j0
+    const int width = chunks * PER + PER + rows - 1;
+    const int64_t nearest = q_start + i0 + rows - 1 - j0 + PER;
+    const auto value = [&](int x) {
+        const int row = relpos_row(nearest - x, borders, rp.buckets, rp.two_sided);
+        return row < 0 ? -INFINITY : column[row];
+    };
+    if constexpr (sizeof(T) == 2) {
+        for (int x = 2 * threadIdx.x; x < width + 1; x += 2 * kBiasBlock) {
+            const uint32_t a = f32_to_bf16_bits(value(x)), b = f32_to_bf16_bits(value(x + 1)), c = f32_to_bf16_bits(value(x + 2));
+            line[x / 2] = a | b << 16;
+            line[MOST / 2 + x / 2] = b | c << 16;
         }
-        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
-        if (lane == 0) partial[part * rows + r] = sum;
+    } else {
+        for (int x = threadIdx.x; x < width; x += kBiasBlock) line[x] = __float_as_uint(value(x));
+    }
+    __syncthreads();
+    // a row's chunks side by side, and as many rows side by side as the workgroup has threads for
+    int wide = 1;
+    while (wide < chunks + 1 && wide < kBiasBlock) wide <<= 1;
+    T* const base = out + h * head_stride + i0 * row_stride + j0;
+    for (int r = threadIdx.x / wide; r < rows; r += kBiasBlock / wide) {
+        T* const row = base + r * row_stride;
+        const int cut = (int)(((uintptr_t)row & 15) / sizeof(T));      // keys by which the row's first aligned chunk begins before it
+        const int64_t left = lk - j0;
+        const int end = (int)min(left, (int64_t)chunks * PER);         // the workgroup's keys are [0, end) of the row
+        for (int c = threadIdx.x % wide; c * PER - cut < end; c += wide) {
+            const int j = c * PER - cut, x = j + PER + rows - 1 - r;
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = sizeof(T) == 4 ? line[x + i] : x % 2 ? line[MOST / 2 + x / 2 + i] : line[x / 2 + i];
+            if (j >= 0 && j + PER <= end) {
+                *reinterpret_cast<uint4*>(row + j) = make_uint4(v[0], v[1], v[2], v[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (j + i >= 0 && j + i < end) {
+                        if constexpr (sizeof(T) == 2) row[j + i] = (T)(v[i / 2] >> (16 * (i % 2)));
+                        else row[j + i] = __uint_as_float(v[i]);
+                    }
+            }
+        }
     }
 }
 
-// grad_table[r][h] = the partial sums of head h, batch by batch and stretch by stretch
-__global__ __launch_bounds__(256) void relpos_bias_join_kernel(const double* __restrict__ partial, int rows, int heads, int64_t batch,
-                                                               int64_t stretches, float* __restrict__ grad_table) {
-    const int e = blockIdx.x * 256 + threadIdx.x;
-    if (e >= rows * heads) return;
-    const int r = e / heads, h = e % heads;
-    double sum = 0;
-    for (int64_t b = 0; b < batch; ++b)
-        for (int64_t s = 0; s < stretches; ++s) sum += partial[((b * heads + h) * stretches + s) * rows + r];
-    grad_table[e] = (float)sum;
+// The gradient's sums run along the diagonals: a wavefront takes 64 blocks of 8 x 8 pairs side by side, a block a lane, and
+// walks down the diagonal with them, so that a lane adds the same 15 diagonals all the way, in registers, and what is not seen
+// (later keys of a one-sided bias) is a matter of whole diagonals: they are dropped behind the walk, whatever they hold.  Bound
+// by the loads: 8 rows of 16 or 32 bytes a lane in flight, the next step's under this one's additions.
+constexpr int kGradBlock = 1 << 3, kGradWaves = 4, kGradSteps = 16;
+constexpr int kGradDiagonals = 64 * kGradBlock + kGradBlock;            // of a wavefront (the last one unused)
+
+template <typename T>
+struct GradBlock {
+    static constexpr int VECS = kGradBlock * sizeof(T) / 16;           // 16-byte loads of a block's row
+    typedef uint32_t Vec __attribute__((ext_vector_type(4)));
+    Vec raw[kGradBlock][VECS];
+    // the block at `at`, of which `rows` x `cols` pairs exist
+    __device__ __forceinline__ void load(const T* at, int64_t row_stride, int rows, int cols) {
+        if (rows >= kGradBlock && cols >= kGradBlock) {
+#pragma unroll
+            for (int i = 0; i < kGradBlock; ++i)
+#pragma unroll
+                for (int v = 0; v < VECS; ++v)      // rows are aligned to their elements only
+                    __builtin_memcpy(&raw[i][v], at + i * row_stride + v * (16 / sizeof(T)), 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kGradBlock; ++i)
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) raw[i][v] = Vec{0, 0, 0, 0};
+            if (rows > 0 && cols > 0) {
+#pragma unroll
+                for (int i = 0; i < kGradBlock; ++i)
+#pragma unroll
+                    for (int j = 0; j < kGradBlock; ++j)
+                        if (i < rows && j < cols) {
+                            const int per = 16 / sizeof(T), k = j % per;
+                            if constexpr (sizeof(T) == 2) raw[i][j / per][k / 2] |= (uint32_t)at[i * row_stride + j] << (16 * (k % 2));
+                            else raw[i][j / per][k] = __float_as_uint(at[i * row_stride + j]);
+                        }
+            }
+        }
+    }
+    __device__ __forceinline__ float value(int i, int j) const {
+        const int per = 16 / sizeof(T), k = j % per, word = sizeof(T) == 2 ? k / 2 : k;
+        const uint32_t u = raw[i][j / per][word];
+        return __uint_as_float(sizeof(T) == 4 ? u : k % 2 ? u & 0xffff0000u : u << 16);
+    }
+};
+
+struct GradArgs {
+    Relpos rp;
+    int64_t lq, lk, row, head, bat, q_start;
+    int64_t blocks_q, blocks_k;            // 8 x 8 blocks down and across
+    int64_t first_band;                    // block diagonal (block column - block row) of band 0's lane 0
+    int32_t bands, segments, steps;        // of 64 block diagonals; of `steps` block rows
+    int32_t heads;
+    double* partial;                       // [batch][heads][bands][segments][table rows]
+};
+
+template <typename T>
+__global__ __launch_bounds__(kGradWaves * 64) void relpos_bias_bwd_kernel(GradArgs a, const T* __restrict__ grad) {
+    __shared__ double diag[kGradWaves][kGradDiagonals], eights[kGradWaves][kGradDiagonals / 8];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t job = (int64_t)blockIdx.x * kGradWaves + wave, jobs = (int64_t)a.bands * a.segments;
+    const bool have = job < jobs;
+    const int64_t band0 = a.first_band + job / a.segments * 64, seg0 = job % a.segments * a.steps;
+    const int64_t kd = band0 + lane;                                   // the lane's block diagonal
+    float acc[2 * kGradBlock - 1];
+#pragma unroll
+    for (int d = 0; d < 2 * kGradBlock - 1; ++d) acc[d] = 0.f;
+    if (have) {
+        // block rows in which some lane has a block
+        const int64_t from = max(seg0, -(band0 + 63)), to = min(min(seg0 + a.steps, a.blocks_q), a.blocks_k - band0);
+        // a one-sided bias sees nothing of a block whose keys are all later
+        const bool seen = a.rp.two_sided || kd * kGradBlock - (kGradBlock - 1) <= a.q_start;
+        const T* const g = grad + blockIdx.z * a.bat + blockIdx.y * a.head;
+        GradBlock<T> cur, next;
+        const auto fetch = [&](GradBlock<T>& b, int64_t row) {
+            const int64_t col = row + kd, i = row * kGradBlock, j = col * kGradBlock;
+            const bool in = seen && row < to && col >= 0 && col < a.blocks_k;
+            b.load(g + i * a.row + j, a.row, in ? (int)min(a.lq - i, (int64_t)kGradBlock) : 0, in ? (int)min(a.lk - j, (int64_t)kGradBlock) : 0);
+        };
+        const auto add = [&](const GradBlock<T>& b) {
+#pragma unroll
+            for (int i = 0; i < kGradBlock; ++i)
+#pragma unroll
+                for (int j = 0; j < kGradBlock; ++j) acc[j - i + kGradBlock - 1] += b.value(i, j);
+        };
+        if (from < to) fetch(cur, from);
+        for (int64_t row = from; row < to; row += 2) {                 // blocks past the end are zeros
+            fetch(next, row + 1);
+            add(cur);
+            fetch(cur, row + 2);
+            add(next);
+        }
+    }
+    // diagonals (j - i) of the wavefront from band0 * 8 - 7 on: neighbours share seven of their fifteen
+    double* const d = diag[wave];
+#pragma unroll
+    for (int k = 0; k < kGradBlock; ++k) d[kGradBlock * lane + k] = acc[k];
+    if (lane == 0)
+        for (int k = 0; k < kGradBlock; ++k) d[64 * kGradBlock + k] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = kGradBlock; k < 2 * kGradBlock - 1; ++k) d[kGradBlock * lane + k] += acc[k];
+    __syncthreads();
+    // A bucket is a stretch of diagonals: its single ones at both ends, and sums of eight in between.  (A NaN where nothing is seen
+    // stays in its own sums: a seen bucket takes no part of a group of eight that it does not hold whole.)
+    for (int e = lane; e < kGradDiagonals / 8; e += 64) {
+        double sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += d[8 * e + k];
+        eights[wave][e] = sum;
+    }
+    __syncthreads();
+    if (!have) return;
+    const int rows = a.rp.rows();
+    double* const out = a.partial + (((int64_t)blockIdx.z * a.heads + blockIdx.y) * jobs + job) * rows;
+    const int64_t zero = band0 * kGradBlock - (kGradBlock - 1);        // the diagonal d[0] is
+    for (int r = lane; r < rows; r += 64) {
+        const bool later = r >= a.rp.buckets;
+        const int b = later ? r - a.rp.buckets : r;
+        const int64_t near = b ? a.rp.borders[b - 1] : later ? 1 : 0, far = b + 1 < a.rp.buckets ? a.rp.borders[b] : int64_t(1) << 40;
+        // distance q_start - diagonal in [near, far), or its negative for later keys
+        const int64_t lo = later ? a.q_start + near : a.q_start - far + 1, hi = later ? a.q_start + far : a.q_start - near + 1;
+        int x = (int)min(max(lo - zero, int64_t(0)), (int64_t)kGradDiagonals);
+        const int end = (int)min(max(hi - zero, int64_t(0)), (int64_t)kGradDiagonals);
+        double sum = 0;
+        while (x < end && x % 8) sum += d[x++];
+        for (; x + 8 <= end; x += 8) sum += eights[wave][x / 8];
+        while (x < end) sum += d[x++];
+        out[r] = sum;
+    }
+}
+
+// grad_table[r][h] = the sum over the wavefronts' parts, a workgroup a head: its wavefronts take a part each in turn, lanes the rows
+__global__ __launch_bounds__(1024) void relpos_bias_join_kernel(const double* __restrict__ partial, int rows, int heads, int64_t batch,
+                                                                int64_t jobs, float* __restrict__ grad_table) {
+    __shared__ double part[16][2 * BP_RELPOS_MAX_BUCKETS];
+    const int h = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (int r = lane; r < rows; r += 64) {
+        double sum = 0;
+        for (int64_t b = 0; b < batch; ++b)
+            for (int64_t s = wave; s < jobs; s += 16) sum += partial[((b * heads + h) * jobs + s) * rows + r];
+        part[wave][r] = sum;
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < rows; r += 1024) {
+        double sum = 0;
+        for (int w = 0; w < 16; ++w) sum += part[w][r];
+        grad_table[(int64_t)r * heads + h] = (float)sum;
+    }
 }
 
 // One thread an element; the row-wise rule takes a workgroup a row.
@@ -174,7 +329,24 @@ int check_grid(int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t row
     *out = Grid4{batch, lq, lk, row, head, bat, heads};
     return BP_OK;
 }
-int64_t grad_stretches(int64_t lq) { return ceil_div(lq, kGradRows); }
+
+// Bands and segments of the walk.  Segments of 16 steps (128 queries) where those make 4,096 wavefronts or more, shorter ones in
+// smaller launches.
+int grad_plan(const Relpos& r, int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t q_start, GradArgs* a) {
+    a->blocks_q = ceil_div(lq, kGradBlock);
+    a->blocks_k = ceil_div(lk, kGradBlock);
+    a->first_band = -(a->blocks_q - 1);
+    int64_t last = a->blocks_k - 1;
+    if (!r.two_sided) last = std::min(last, (q_start + kGradBlock - 1) >> 3);            // rounded down
+    const int64_t bands = lq == 0 || lk == 0 || last < a->first_band ? 0 : ceil_div(last - a->first_band + 1, 64);
+    a->steps = kGradSteps;
+    while (a->steps > 2 && batch * heads * bands * ceil_div(a->blocks_q, a->steps) < 4096) a->steps /= 2;
+    const int64_t segments = ceil_div(a->blocks_q, a->steps);
+    if (bands * segments >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
+    a->bands = (int32_t)bands;
+    a->segments = (int32_t)segments;
+    return BP_OK;
+}
 
 }  // namespace
 }  // namespace bp
@@ -214,13 +386,20 @@ BP_EXPORT int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_
     if (heads == 0 || lq == 0 || lk == 0) return BP_OK;
     if (!table || !out) return fail(BP_ERR_INVALID_ARG, "NULL pointer");
     if (((uintptr_t)table & 3) || (uintptr_t)out % elem_bytes(out_dtype)) return fail(BP_ERR_INVALID_ARG, "table or out is not aligned to its element");
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(heads * lq * lk, 256), 1 << 20));
+    // a workgroup's keys: a chunk a thread; fewer where there are too few workgroups for the chip
+    const int per = 16 / (int)elem_bytes(out_dtype);
+    const int64_t row_blocks = ceil_div(lq, kBiasRows), all_chunks = ceil_div(lk, per);
+    int chunks = kBiasChunks;
+    while (chunks > 32 && heads * row_blocks * ceil_div(all_chunks, chunks) < 512) chunks /= 2;
+    const int64_t tiles = ceil_div(all_chunks, chunks);
+    if (tiles * row_blocks >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
+    const dim3 grid((unsigned)(tiles * row_blocks), (unsigned)heads);
     if (out_dtype == BP_F32)
-        BP_LAUNCH(K_RELPOS_FWD, relpos_bias_fwd_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, r, table, heads, lq, lk, q_start,
-                  (float*)out, g.row, g.head);
+        BP_LAUNCH(K_RELPOS_FWD, relpos_bias_fwd_kernel<float>, grid, dim3(kBiasBlock), 0, (hipStream_t)stream, r, table, heads, lq, lk, q_start,
+                  (float*)out, g.row, g.head, chunks, tiles);
     else
-        BP_LAUNCH(K_RELPOS_FWD, relpos_bias_fwd_kernel<uint16_t>, grid, dim3(256), 0, (hipStream_t)stream, r, table, heads, lq, lk, q_start,
-                  (uint16_t*)out, g.row, g.head);
+        BP_LAUNCH(K_RELPOS_FWD, relpos_bias_fwd_kernel<uint16_t>, grid, dim3(kBiasBlock), 0, (hipStream_t)stream, r, table, heads, lq, lk,
+                  q_start, (uint16_t*)out, g.row, g.head, chunks, tiles);
     return BP_OK;
 }
 
@@ -230,7 +409,13 @@ BP_EXPORT int bp_relpos_bias_bwd_workspace_bytes(const bp_relpos* rp, int64_t ba
     if (!bytes) return fail(BP_ERR_INVALID_ARG, "bytes is NULL");
     BP_TRY(check_relpos(rp, &r));
     BP_TRY(check_grid(batch, heads, lq, lk, 0, 0, 0, 0, &g));
-    *bytes = (size_t)(batch * heads * grad_stretches(lq) * r.rows()) * sizeof(double);
+    GradArgs a{};
+    const int rows = r.rows();
+    r.two_sided = 1;                                   // room for every q_start: as if all keys were seen
+    BP_TRY(grad_plan(r, batch, heads, lq, lk, 0, &a));
+    // shorter segments come to less than twice 4,096 wavefronts
+    const int64_t walks = batch * heads * a.bands;
+    *bytes = (size_t)(std::max(walks * ceil_div(a.blocks_q, kGradSteps), std::min<int64_t>(8192, walks * ceil_div(a.blocks_q, 2))) * rows) * sizeof(double);
     return BP_OK;
 }
 
@@ -251,19 +436,26 @@ BP_EXPORT int bp_relpos_bias_bwd(const bp_relpos* rp, const void* grad_out, int3
     BP_TRY(bp_relpos_bias_bwd_workspace_bytes(rp, batch, heads, lq, lk, &need));
     if (need && (!workspace || ((uintptr_t)workspace & 255))) return fail(BP_ERR_INVALID_ARG, "workspace NULL or not 256-byte aligned");
     if (workspace_bytes < need) return fail(BP_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < required %zu bytes", workspace_bytes, need);
-    double* const partial = (double*)workspace;
-    const int64_t stretches = grad_stretches(lq);
-    if (batch && lq) {
-        const dim3 grid((unsigned)stretches, (unsigned)heads, (unsigned)batch);
+    GradArgs a{};
+    BP_TRY(grad_plan(r, batch, heads, lq, lk, q_start, &a));
+    a.rp = r;
+    a.lq = lq;
+    a.lk = lk;
+    a.row = g.row;
+    a.head = g.head;
+    a.bat = g.bat;
+    a.q_start = q_start;
+    a.heads = heads;
+    a.partial = (double*)workspace;
+    const int64_t jobs = (int64_t)a.bands * a.segments;
+    if (batch && jobs) {
+        const dim3 grid((unsigned)ceil_div(jobs, kGradWaves), (unsigned)heads, (unsigned)batch), block(kGradWaves * 64);
         if (grad_dtype == BP_F32)
-            BP_LAUNCH(K_RELPOS_BWD, relpos_bias_bwd_kernel<float>, grid, dim3(64), 0, stream, r, (const float*)grad_out, lq, lk, g.row, g.head,
-                      g.bat, q_start, partial);
+            BP_LAUNCH(K_RELPOS_BWD, relpos_bias_bwd_kernel<float>, grid, block, 0, stream, a, (const float*)grad_out);
         else
-            BP_LAUNCH(K_RELPOS_BWD, relpos_bias_bwd_kernel<uint16_t>, grid, dim3(64), 0, stream, r, (const uint16_t*)grad_out, lq, lk, g.row,
-                      g.head, g.bat, q_start, partial);
+            BP_LAUNCH(K_RELPOS_BWD, relpos_bias_bwd_kernel<uint16_t>, grid, block, 0, stream, a, (const uint16_t*)grad_out);
     }
-    BP_LAUNCH(K_RELPOS_JOIN, relpos_bias_join_kernel, dim3((unsigned)ceil_div((int64_t)r.rows() * heads, 256)), dim3(256), 0, stream, partial,
-              r.rows(), heads, lq ? batch : 0, stretches, grad_table);
+    BP_LAUNCH(K_RELPOS_JOIN, relpos_bias_join_kernel, dim3((unsigned)heads), dim3(1024), 0, stream, a.partial, r.rows(), heads, batch, jobs, grad_table);
     return BP_OK;
 }
 
