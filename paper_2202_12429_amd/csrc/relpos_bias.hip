@@ -83,10 +83,12 @@ __global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, 
         return row < 0 ? -INFINITY : column[row];
     };
     if constexpr (sizeof(T) == 2) {
-        for (int x = 2 * threadIdx.x; x < width + 1; x += 2 * kBiasBlock) {
-            const uint32_t a = f32_to_bf16_bits(value(x)), b = f32_to_bf16_bits(value(x + 1)), c = f32_to_bf16_bits(value(x + 2));
-            line[x / 2] = a | b << 16;
-            line[MOST / 2 + x / 2] = b | c << 16;
+        uint16_t* const even = (uint16_t*)line;
+        uint16_t* const odd = (uint16_t*)(line + MOST / 2);
+        for (int x = threadIdx.x; x < width; x += kBiasBlock) {
+            const uint16_t v = (uint16_t)f32_to_bf16_bits(value(x));
+            even[x] = v;
+            if (x) odd[x - 1] = v;
         }
     } else {
         for (int x = threadIdx.x; x < width; x += kBiasBlock) line[x] = __float_as_uint(value(x));
@@ -121,55 +123,65 @@ __global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, 
     }
 }
 
-// The gradient's sums run along the diagonals: a wavefront takes 64 blocks of 8 x 8 pairs side by side, a block a lane, and
-// walks down the diagonal with them, so that a lane adds the same 15 diagonals all the way, in registers, and what is not seen
-// (later keys of a one-sided bias) is a matter of whole diagonals: they are dropped behind the walk, whatever they hold.  Bound
-// by the loads: 8 rows of 16 or 32 bytes a lane in flight, the next step's under this one's additions.
-constexpr int kGradBlock = 1 << 3, kGradWaves = 4, kGradSteps = 16;
-constexpr int kGradDiagonals = 64 * kGradBlock + kGradBlock;            // of a wavefront (the last one unused)
+// The gradient's sums run along the diagonals: a wavefront takes 64 blocks of NB x NB pairs side by side, a block a lane (NB
+// keys are 16 bytes), and walks down the diagonal with them, so that a lane adds the same 2 NB - 1 diagonals all the way, in
+// registers, and what is not seen (later keys of a one-sided bias) is a matter of whole diagonals: they are dropped behind the
+// walk, whatever they hold.  Bound by the loads: NB rows of 16 bytes a lane in flight, the next step's under this one's additions.
+constexpr int kGradWaves = 4;
 
 template <typename T>
 struct GradBlock {
-    static constexpr int VECS = kGradBlock * sizeof(T) / 16;           // 16-byte loads of a block's row
+    static constexpr int NB = 16 / sizeof(T), STEPS = 128 / NB, DIAGONALS = 64 * NB + 8;      // (the last ones unused)
     typedef uint32_t Vec __attribute__((ext_vector_type(4)));
-    Vec raw[kGradBlock][VECS];
-    // the block at `at`, of which `rows` x `cols` pairs exist
-    __device__ __forceinline__ void load(const T* at, int64_t row_stride, int rows, int cols) {
-        if (rows >= kGradBlock && cols >= kGradBlock) {
+    Vec raw[NB];
+    // The block at `at`, of which `rows` x `cols` pairs exist; `left`: elements from `at` to the end of the array.  A row's 16 bytes
+    // are read as long as they lie in the array, and cut after that.
+    __device__ __forceinline__ void load(const T* at, int64_t row_stride, int64_t left, int rows, int cols) {
+        // zeros first, for every lane: written behind the branch they would have to wait for the loads of the lanes inside it
 #pragma unroll
-            for (int i = 0; i < kGradBlock; ++i)
+        for (int i = 0; i < NB; ++i) raw[i] = Vec{0, 0, 0, 0};
+        if (rows >= NB && cols >= NB) {
 #pragma unroll
-                for (int v = 0; v < VECS; ++v)      // rows are aligned to their elements only
-                    __builtin_memcpy(&raw[i][v], at + i * row_stride + v * (16 / sizeof(T)), 16);
-        } else {
+            for (int i = 0; i < NB; ++i) __builtin_memcpy(&raw[i], at + i * row_stride, 16);           // aligned to their elements only
+        }
+        if (rows <= 0 || cols <= 0 || (rows >= NB && cols >= NB)) return;
 #pragma unroll
-            for (int i = 0; i < kGradBlock; ++i)
+        for (int i = 0; i < NB; ++i) {
+            if (i >= rows) continue;
+            const T* const row = at + i * row_stride;
+            if (i * row_stride + NB <= left) {
+                __builtin_memcpy(&raw[i], row, 16);
+            } else {
+                uint64_t lo = 0, hi = 0;                               // the array's last few elements, one by one
+#pragma unroll 1
+                for (int j = 0; j < cols; ++j) {
+                    uint32_t bits;
+                    if constexpr (sizeof(T) == 2) bits = row[j];
+                    else bits = __float_as_uint(row[j]);
+                    const uint64_t v = (uint64_t)bits << (j % (NB / 2) * (8 * sizeof(T)));
+                    if (j < NB / 2) lo |= v;
+                    else hi |= v;
+                }
+                raw[i] = Vec{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+            }
 #pragma unroll
-                for (int v = 0; v < VECS; ++v) raw[i][v] = Vec{0, 0, 0, 0};
-            if (rows > 0 && cols > 0) {
-#pragma unroll
-                for (int i = 0; i < kGradBlock; ++i)
-#pragma unroll
-                    for (int j = 0; j < kGradBlock; ++j)
-                        if (i < rows && j < cols) {
-                            const int per = 16 / sizeof(T), k = j % per;
-                            if constexpr (sizeof(T) == 2) raw[i][j / per][k / 2] |= (uint32_t)at[i * row_stride + j] << (16 * (k % 2));
-                            else raw[i][j / per][k] = __float_as_uint(at[i * row_stride + j]);
-                        }
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (sizeof(T) == 2) raw[i][w] &= (2 * w < cols ? 0xffffu : 0u) | (2 * w + 1 < cols ? 0xffff0000u : 0u);
+                else raw[i][w] = w < cols ? raw[i][w] : 0u;
             }
         }
     }
     __device__ __forceinline__ float value(int i, int j) const {
-        const int per = 16 / sizeof(T), k = j % per, word = sizeof(T) == 2 ? k / 2 : k;
-        const uint32_t u = raw[i][j / per][word];
-        return __uint_as_float(sizeof(T) == 4 ? u : k % 2 ? u & 0xffff0000u : u << 16);
+        if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i][j]);
+        else return __uint_as_float(j % 2 ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16);
     }
 };
 
 struct GradArgs {
     Relpos rp;
     int64_t lq, lk, row, head, bat, q_start;
-    int64_t blocks_q, blocks_k;            // 8 x 8 blocks down and across
+    int64_t blocks_q, blocks_k;            // blocks down and across
+    int64_t span;                          // elements from the first pair to the last one, and one more
     int64_t first_band;                    // block diagonal (block column - block row) of band 0's lane 0
     int32_t bands, segments, steps;        // of 64 block diagonals; of `steps` block rows
     int32_t heads;
@@ -178,97 +190,110 @@ struct GradArgs {
 
 template <typename T>
 __global__ __launch_bounds__(kGradWaves * 64) void relpos_bias_bwd_kernel(GradArgs a, const T* __restrict__ grad) {
-    __shared__ double diag[kGradWaves][kGradDiagonals], eights[kGradWaves][kGradDiagonals / 8];
+    typedef GradBlock<T> B;
+    constexpr int NB = B::NB;
+    __shared__ double diag[kGradWaves][B::DIAGONALS], eights[kGradWaves][B::DIAGONALS / 8], more[kGradWaves][B::DIAGONALS / 64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t job = (int64_t)blockIdx.x * kGradWaves + wave, jobs = (int64_t)a.bands * a.segments;
+    // Segments of a head differ in work (the corners of the grid, a one-sided bias's later keys), and a CU gets workgroups at a
+    // stride that often is a multiple of a head's: every head begins at another of them.
+    const uint32_t turn = (uint32_t)(((uint64_t)(blockIdx.y + blockIdx.z * gridDim.y) * 2654435769u >> 7) % gridDim.x);
+    const uint32_t group = blockIdx.x + turn < gridDim.x ? blockIdx.x + turn : blockIdx.x + turn - gridDim.x;
+    const int64_t job = (int64_t)group * kGradWaves + wave, jobs = (int64_t)a.bands * a.segments;
     const bool have = job < jobs;
     const int64_t band0 = a.first_band + job / a.segments * 64, seg0 = job % a.segments * a.steps;
     const int64_t kd = band0 + lane;                                   // the lane's block diagonal
-    float acc[2 * kGradBlock - 1];
+    float acc[2 * NB - 1];
 #pragma unroll
-    for (int d = 0; d < 2 * kGradBlock - 1; ++d) acc[d] = 0.f;
+    for (int d = 0; d < 2 * NB - 1; ++d) acc[d] = 0.f;
     if (have) {
         // block rows in which some lane has a block
         const int64_t from = max(seg0, -(band0 + 63)), to = min(min(seg0 + a.steps, a.blocks_q), a.blocks_k - band0);
         // a one-sided bias sees nothing of a block whose keys are all later
-        const bool seen = a.rp.two_sided || kd * kGradBlock - (kGradBlock - 1) <= a.q_start;
-        const T* const g = grad + blockIdx.z * a.bat + blockIdx.y * a.head;
-        GradBlock<T> cur, next;
-        const auto fetch = [&](GradBlock<T>& b, int64_t row) {
-            const int64_t col = row + kd, i = row * kGradBlock, j = col * kGradBlock;
+        const bool seen = a.rp.two_sided || kd * NB - (NB - 1) <= a.q_start;
+        const int64_t base = blockIdx.z * a.bat + blockIdx.y * a.head;
+        B cur;
+        const auto fetch = [&](B& b, int64_t row) {
+            const int64_t col = row + kd, i = row * NB, j = col * NB;
             const bool in = seen && row < to && col >= 0 && col < a.blocks_k;
-            b.load(g + i * a.row + j, a.row, in ? (int)min(a.lq - i, (int64_t)kGradBlock) : 0, in ? (int)min(a.lk - j, (int64_t)kGradBlock) : 0);
+            const int64_t at = base + i * a.row + j;
+            b.load(grad + at, a.row, a.span - at, in ? (int)min(a.lq - i, (int64_t)NB) : 0, in ? (int)min(a.lk - j, (int64_t)NB) : 0);
         };
-        const auto add = [&](const GradBlock<T>& b) {
+        const auto add = [&](const B& b) {
 #pragma unroll
-            for (int i = 0; i < kGradBlock; ++i)
+            for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int j = 0; j < kGradBlock; ++j) acc[j - i + kGradBlock - 1] += b.value(i, j);
+                for (int j = 0; j < NB; ++j) acc[j - i + NB - 1] += b.value(i, j);
         };
-        if (from < to) fetch(cur, from);
-        for (int64_t row = from; row < to; row += 2) {                 // blocks past the end are zeros
-            fetch(next, row + 1);
+        for (int64_t row = from; row < to; ++row) {
+            fetch(cur, row);
             add(cur);
-            fetch(cur, row + 2);
-            add(next);
         }
     }
-    // diagonals (j - i) of the wavefront from band0 * 8 - 7 on: neighbours share seven of their fifteen
+    // diagonals (j - i) of the wavefront from band0 * NB - (NB - 1) on: neighbours share NB - 1 of theirs
     double* const d = diag[wave];
 #pragma unroll
-    for (int k = 0; k < kGradBlock; ++k) d[kGradBlock * lane + k] = acc[k];
-    if (lane == 0)
-        for (int k = 0; k < kGradBlock; ++k) d[64 * kGradBlock + k] = 0;
+    for (int k = 0; k < NB; ++k) d[NB * lane + k] = acc[k];
+    if (lane < 8) d[64 * NB + lane] = 0;
     __syncthreads();
 #pragma unroll
-    for (int k = kGradBlock; k < 2 * kGradBlock - 1; ++k) d[kGradBlock * lane + k] += acc[k];
+    for (int k = NB; k < 2 * NB - 1; ++k) d[NB * lane + k] += acc[k];
     __syncthreads();
-    // A bucket is a stretch of diagonals: its single ones at both ends, and sums of eight in between.  (A NaN where nothing is seen
-    // stays in its own sums: a seen bucket takes no part of a group of eight that it does not hold whole.)
-    for (int e = lane; e < kGradDiagonals / 8; e += 64) {
+    // A bucket is a stretch of diagonals: single ones at both ends, sums of eight and of sixty-four in between, so that no lane
+    // adds more than 36 values one behind the other.  (A NaN where nothing is seen stays in its own sums: a seen bucket takes no
+    // part of a sum that it does not hold whole.)
+    for (int e = lane; e < B::DIAGONALS / 8; e += 64) {
         double sum = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum += d[8 * e + k];
         eights[wave][e] = sum;
     }
     __syncthreads();
+    if (lane < B::DIAGONALS / 64) {
+        double sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += eights[wave][8 * lane + k];
+        more[wave][lane] = sum;
+    }
+    __syncthreads();
     if (!have) return;
     const int rows = a.rp.rows();
     double* const out = a.partial + (((int64_t)blockIdx.z * a.heads + blockIdx.y) * jobs + job) * rows;
-    const int64_t zero = band0 * kGradBlock - (kGradBlock - 1);        // the diagonal d[0] is
+    const int64_t zero = band0 * NB - (NB - 1);                        // the diagonal d[0] is
     for (int r = lane; r < rows; r += 64) {
         const bool later = r >= a.rp.buckets;
         const int b = later ? r - a.rp.buckets : r;
         const int64_t near = b ? a.rp.borders[b - 1] : later ? 1 : 0, far = b + 1 < a.rp.buckets ? a.rp.borders[b] : int64_t(1) << 40;
         // distance q_start - diagonal in [near, far), or its negative for later keys
         const int64_t lo = later ? a.q_start + near : a.q_start - far + 1, hi = later ? a.q_start + far : a.q_start - near + 1;
-        int x = (int)min(max(lo - zero, int64_t(0)), (int64_t)kGradDiagonals);
-        const int end = (int)min(max(hi - zero, int64_t(0)), (int64_t)kGradDiagonals);
+        int x = (int)min(max(lo - zero, int64_t(0)), (int64_t)B::DIAGONALS);
+        const int end = (int)min(max(hi - zero, int64_t(0)), (int64_t)B::DIAGONALS);
         double sum = 0;
         while (x < end && x % 8) sum += d[x++];
+        for (; x + 8 <= end && x % 64; x += 8) sum += eights[wave][x / 8];
+        for (; x + 64 <= end; x += 64) sum += more[wave][x / 64];
         for (; x + 8 <= end; x += 8) sum += eights[wave][x / 8];
         while (x < end) sum += d[x++];
         out[r] = sum;
     }
 }
 
-// grad_table[r][h] = the sum over the wavefronts' parts, a workgroup a head: its wavefronts take a part each in turn, lanes the rows
-__global__ __launch_bounds__(1024) void relpos_bias_join_kernel(const double* __restrict__ partial, int rows, int heads, int64_t batch,
-                                                                int64_t jobs, float* __restrict__ grad_table) {
-    __shared__ double part[16][2 * BP_RELPOS_MAX_BUCKETS];
-    const int h = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int r = lane; r < rows; r += 64) {
-        double sum = 0;
+// grad_table[r][h] = the sum over the wavefronts' parts: a workgroup 16 rows of a head, 64 shares of the parts side by side
+constexpr int kJoinRows = 16, kJoinShares = 64;
+__global__ __launch_bounds__(kJoinRows * kJoinShares) void relpos_bias_join_kernel(const double* __restrict__ partial, int rows, int heads,
+                                                                                   int64_t batch, int64_t jobs, float* __restrict__ grad_table) {
+    __shared__ double part[kJoinShares][kJoinRows];
+    const int h = blockIdx.x, c = threadIdx.x % kJoinRows, r = blockIdx.y * kJoinRows + c, share = threadIdx.x / kJoinRows;
+    double sum = 0;
+    if (r < rows)
         for (int64_t b = 0; b < batch; ++b)
-            for (int64_t s = wave; s < jobs; s += 16) sum += partial[((b * heads + h) * jobs + s) * rows + r];
-        part[wave][r] = sum;
-    }
+            for (int64_t s = share; s < jobs; s += kJoinShares) sum += partial[((b * heads + h) * jobs + s) * rows + r];
+    part[share][c] = sum;
     __syncthreads();
-    for (int r = threadIdx.x; r < rows; r += 1024) {
-        double sum = 0;
-        for (int w = 0; w < 16; ++w) sum += part[w][r];
-        grad_table[(int64_t)r * heads + h] = (float)sum;
+    for (int off = kJoinShares / 2; off >= 1; off >>= 1) {
+        if (share < off) part[share][c] += part[share + off][c];
+        __syncthreads();
     }
+    if (share == 0 && r < rows) grad_table[(int64_t)r * heads + h] = (float)part[0][c];
 }
 
 // One thread an element; the row-wise rule takes a workgroup a row.
@@ -330,17 +355,19 @@ int check_grid(int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t row
     return BP_OK;
 }
 
-// Bands and segments of the walk.  Segments of 16 steps (128 queries) where those make 4,096 wavefronts or more, shorter ones in
-// smaller launches.
-int grad_plan(const Relpos& r, int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t q_start, GradArgs* a) {
-    a->blocks_q = ceil_div(lq, kGradBlock);
-    a->blocks_k = ceil_div(lk, kGradBlock);
+// Bands and segments of the walk.  Segments of 128 queries where those make 4,096 wavefronts or more, shorter ones in smaller
+// launches.
+constexpr int kGradEnough = 4096;
+int grad_plan(const Relpos& r, int32_t dtype, int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t q_start, GradArgs* a) {
+    const int block = 16 / (int)elem_bytes(dtype), shift = dtype == BP_F32 ? 2 : 3;
+    a->blocks_q = ceil_div(lq, block);
+    a->blocks_k = ceil_div(lk, block);
     a->first_band = -(a->blocks_q - 1);
     int64_t last = a->blocks_k - 1;
-    if (!r.two_sided) last = std::min(last, (q_start + kGradBlock - 1) >> 3);            // rounded down
+    if (!r.two_sided) last = std::min(last, (q_start + block - 1) >> shift);            // rounded down
     const int64_t bands = lq == 0 || lk == 0 || last < a->first_band ? 0 : ceil_div(last - a->first_band + 1, 64);
-    a->steps = kGradSteps;
-    while (a->steps > 2 && batch * heads * bands * ceil_div(a->blocks_q, a->steps) < 4096) a->steps /= 2;
+    a->steps = 128 / block;
+    while (a->steps > 4 && batch * heads * bands * ceil_div(a->blocks_q, a->steps) < kGradEnough) a->steps /= 2;
     const int64_t segments = ceil_div(a->blocks_q, a->steps);
     if (bands * segments >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
     a->bands = (int32_t)bands;
@@ -409,13 +436,17 @@ BP_EXPORT int bp_relpos_bias_bwd_workspace_bytes(const bp_relpos* rp, int64_t ba
     if (!bytes) return fail(BP_ERR_INVALID_ARG, "bytes is NULL");
     BP_TRY(check_relpos(rp, &r));
     BP_TRY(check_grid(batch, heads, lq, lk, 0, 0, 0, 0, &g));
-    GradArgs a{};
     const int rows = r.rows();
     r.two_sided = 1;                                   // room for every q_start: as if all keys were seen
-    BP_TRY(grad_plan(r, batch, heads, lq, lk, 0, &a));
-    // shorter segments come to less than twice 4,096 wavefronts
-    const int64_t walks = batch * heads * a.bands;
-    *bytes = (size_t)(std::max(walks * ceil_div(a.blocks_q, kGradSteps), std::min<int64_t>(8192, walks * ceil_div(a.blocks_q, 2))) * rows) * sizeof(double);
+    *bytes = 0;
+    for (int32_t dtype : {BP_F32, BP_BF16}) {
+        GradArgs a{};
+        BP_TRY(grad_plan(r, dtype, batch, heads, lq, lk, 0, &a));
+        // (shorter segments come to less than twice the wavefronts that are enough)
+        const int64_t walks = batch * heads * a.bands, block = 16 / (int64_t)elem_bytes(dtype);
+        const int64_t most = std::max(walks * ceil_div(a.blocks_q, 128 / block), std::min<int64_t>(2 * kGradEnough, walks * ceil_div(a.blocks_q, 4)));
+        *bytes = std::max(*bytes, (size_t)(most * rows) * sizeof(double));
+    }
     return BP_OK;
 }
 
@@ -437,13 +468,14 @@ BP_EXPORT int bp_relpos_bias_bwd(const bp_relpos* rp, const void* grad_out, int3
     if (need && (!workspace || ((uintptr_t)workspace & 255))) return fail(BP_ERR_INVALID_ARG, "workspace NULL or not 256-byte aligned");
     if (workspace_bytes < need) return fail(BP_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < required %zu bytes", workspace_bytes, need);
     GradArgs a{};
-    BP_TRY(grad_plan(r, batch, heads, lq, lk, q_start, &a));
+    BP_TRY(grad_plan(r, grad_dtype, batch, heads, lq, lk, q_start, &a));
     a.rp = r;
     a.lq = lq;
     a.lk = lk;
     a.row = g.row;
     a.head = g.head;
     a.bat = g.bat;
+    a.span = batch && heads && lq ? (batch - 1) * g.bat + (heads - 1) * g.head + (lq - 1) * g.row + lk : 0;
     a.q_start = q_start;
     a.heads = heads;
     a.partial = (double*)workspace;
@@ -455,7 +487,8 @@ BP_EXPORT int bp_relpos_bias_bwd(const bp_relpos* rp, const void* grad_out, int3
         else
             BP_LAUNCH(K_RELPOS_BWD, relpos_bias_bwd_kernel<uint16_t>, grid, block, 0, stream, a, (const uint16_t*)grad_out);
     }
-    BP_LAUNCH(K_RELPOS_JOIN, relpos_bias_join_kernel, dim3((unsigned)heads), dim3(1024), 0, stream, a.partial, r.rows(), heads, batch, jobs, grad_table);
+    BP_LAUNCH(K_RELPOS_JOIN, relpos_bias_join_kernel, dim3((unsigned)heads, (unsigned)ceil_div(r.rows(), kJoinRows)),
+              dim3(kJoinRows * kJoinShares), 0, stream, a.partial, r.rows(), heads, batch, jobs, grad_table);
     return BP_OK;
 }
 
