@@ -129,6 +129,7 @@ enum KernelId {
     K_ATTN_BWD,
     K_ATTN_JOIN,
     K_EVICT_SELECT,
+    K_EVICT_MOVE,
     K_NUM_KERNELS
 };
 

@@ -6,7 +6,6 @@
 namespace bp {
 namespace {
 
-constexpr int kEvictBlock = 256;
 constexpr int64_t kMaxLists = int64_t(1) << 24;
 
 struct EvictArgs {
@@ -24,6 +23,12 @@ struct EvictArgs {
     int32_t* evict_slots;
     int64_t list_capacity;
     int64_t* evict_off;
+    int32_t scanned;               // evict_off is there already
+    int32_t split;                 // lists are taken by pieces of kPiece entries, else whole
+    uint32_t parts;                // pieces, or lists
+    struct Choice* choice;         // [parts]
+    uint2* begins;                 // [parts][kStretches]: ties, and entries that leave, of the list before a stretch
+    uint32_t* hist;                // [parts][kDigits][kBins] of lists of several pieces
 };
 
 // The entries [first, first + count) of a list; offsets and lengths that point outside the arrays use nothing there.
@@ -47,119 +52,460 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* scratch) {
-    __syncthreads();
-    scratch[threadIdx.x] = v;
-    __syncthreads();
-    for (int off = kEvictBlock / 2; off >= 1; off >>= 1) {
-        if ((int)threadIdx.x < off) scratch[threadIdx.x] += scratch[threadIdx.x + off];
-        __syncthreads();
+// ---- selection -----------------------------------------------------------------------------------------------------------
+// The weight up to which a list's entries leave is found eleven bits at a time by counting.  A workgroup takes a list, whose keys
+// stay in its registers (up to 32 a thread, so the list is read once; longer ones are read again for every digit); or, where
+// lists are long, a piece of one, and the pieces of a list meet over three launches, each of which adds up the counts that the
+// one before left.  A wavefront's entries lie side by side, 64 a step: its stretch.
+constexpr int kDigits = 3, kBins = 2048, kStretches = 16;
+constexpr int kPieceShift = 15, kPiece = 1 << kPieceShift;        // what 1,024 threads hold
+constexpr int kShift[kDigits] = {21, 10, 0}, kWidth[kDigits] = {11, 11, 10};
+
+constexpr int kFew = 8;           // up to so many leave: found one by one, which takes a barrier each instead of the digits' nine
+
+struct Choice {
+    uint32_t key;             // the largest key that leaves
+    uint32_t ties;            // how many of the entries with that key leave: the earliest
+    int64_t before;           // entries that leave earlier lists
+};
+
+// What a workgroup works on: a list, or a piece of one.
+struct Part {
+    int64_t bag, first;             // the list
+    int32_t count;
+    int32_t begin, end;             // the part's places in it
+    uint32_t first_id, of, number;  // the list's parts
+};
+__device__ __forceinline__ uint32_t first_part(const EvictArgs& a, int64_t bag) {
+    int64_t at = a.bag_off[bag];
+    if (at < 0) at = 0;
+    if (at > a.n) at = a.n;
+    return (uint32_t)(at >> kPieceShift) + (uint32_t)bag;
+}
+__device__ __forceinline__ Part find_part(const EvictArgs& a, uint32_t id) {
+    Part p;
+    p.first = 0;
+    p.count = p.begin = p.end = 0;
+    p.bag = id;
+    p.first_id = id;
+    p.of = 1;
+    p.number = 0;
+    if (id >= a.parts || a.bags == 0) {
+        p.bag = a.bags;
+        return p;
     }
-    const int64_t r = scratch[0];
-    __syncthreads();
-    return r;
+    if (a.split) {                    // the last list that begins no later, 64 lists a step
+        const uint32_t lane = threadIdx.x % 64;
+        uint32_t lo = 0, hi = (uint32_t)a.bags;
+        while (hi - lo > 1) {
+            const uint32_t step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step;
+            lo += __popcll(__ballot(i < hi && first_part(a, i) <= id)) * step;
+            hi = min(hi, lo + step);
+        }
+        p.bag = lo;
+        p.first_id = first_part(a, lo);
+        p.number = id - p.first_id;
+    }
+    int64_t count;
+    list_span(a, p.bag, &p.first, &count);
+    p.count = p.end = (int32_t)count;
+    if (a.split) {
+        p.of = (uint32_t)max(int64_t(1), min((count + kPiece - 1) >> kPieceShift, (int64_t)a.parts - p.first_id));
+        if (p.number >= p.of) {
+            p.begin = p.count;                                    // a number without a piece
+        } else {
+            p.begin = (int32_t)(p.number << kPieceShift);
+            if (p.number + 1 < p.of) p.end = p.begin + kPiece;
+        }
+    }
+    return p;
 }
 
-// A workgroup a list.  The weight up to which entries leave is found eight bits at a time by counting; of the entries that have
-// exactly that weight the earliest leave.
-__global__ __launch_bounds__(kEvictBlock) void evict_kernel(EvictArgs a) {
-    __shared__ int64_t scratch[kEvictBlock];
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t found, rest;
-    __shared__ uint32_t scan[2][kEvictBlock];
-    const int64_t bag = blockIdx.x;
-    int64_t before = 0;
-    for (int64_t b = threadIdx.x; b < bag; b += kEvictBlock) {
-        int64_t f, c;
-        list_span(a, b, &f, &c);
-        before += max(int64_t(0), c - a.budget);
+// Sum over the workgroup of v over the threads before this one, and over all.
+template <int BLOCK>
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* waves, uint32_t* all) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint32_t upto = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t x = __shfl_up(upto, off);
+        if (lane >= off) upto += x;
     }
-    before = block_sum(before, scratch);
-    int64_t first = 0, count = 0;
-    if (bag < a.bags) list_span(a, bag, &first, &count);
-    const int64_t over = max(int64_t(0), count - a.budget);
-    if (threadIdx.x == 0) {
-        if (bag < a.bags) a.kept_len[bag] = (int32_t)(count - over);
-        a.evict_off[bag] = before;
-        if (bag == a.bags - 1) a.evict_off[a.bags] = before + over;
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - v, total = 0;
+#pragma unroll
+    for (int w = 0; w < BLOCK / 64; ++w) {
+        if (w < wave) before += waves[w];
+        total += waves[w];
     }
-    if (bag >= a.bags - 1)                                  // the last list, or none at all
-        for (int64_t e = before + over + threadIdx.x; e < a.list_capacity; e += kEvictBlock) {
-            if (a.evict_ids) a.evict_ids[e] = -1;
-            a.evict_slots[e] = -1;
-        }
-    const int64_t may0 = a.sinks, may1 = count - a.recent;
-    uint32_t prefix = 0, need = (uint32_t)over;            // the need-th smallest key that starts with the bits found so far
-    if (over) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            hist[threadIdx.x] = 0;
-            __syncthreads();
-            for (int64_t e = may0 + threadIdx.x; e < may1; e += kEvictBlock) {
-                const uint32_t key = weight_key(a.weight[first + e]);
-                if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[key >> shift & 255], 1u);
+    *all = total;
+    return before;
+}
+
+// The digit in which the need-th smallest key lies, and how many are left to count in it (into LDS; read behind a barrier).
+template <int BLOCK>
+__device__ __forceinline__ void find_digit(const uint32_t (&c)[kBins / BLOCK], uint32_t need, uint32_t* waves, uint32_t* found, uint32_t* rest) {
+    uint32_t sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < kBins / BLOCK; ++i) sum += c[i];
+    uint32_t before = sum_before<BLOCK>(sum, waves, &all);
+    if (before < need && need <= before + sum) {                   // one thread
+#pragma unroll
+        for (int i = 0; i < kBins / BLOCK; ++i) {
+            if (before < need && need <= before + c[i]) {
+                *found = (kBins / BLOCK) * threadIdx.x + i;
+                *rest = need - before;
             }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                uint32_t left = need, d = 0;
-                while (left > hist[d]) left -= hist[d++];
-                found = d;
-                rest = left;
-            }
-            __syncthreads();
-            prefix |= found << shift;
-            need = rest;
-            __syncthreads();
+            before += c[i];
         }
     }
-    // the kept entries and the others, each in order
-    int64_t kept = 0, gone = 0, ties = 0;
-    for (int64_t e0 = 0; e0 < count; e0 += kEvictBlock) {
-        const int64_t e = e0 + threadIdx.x;
-        const bool may = over && e >= may0 && e < may1;
-        const float w = e < count ? a.weight[first + e] : 0.f;
-        const uint32_t key = weight_key(w);
-        const bool tie = may && key == prefix;
-        int cur = 0;
-        uint32_t all[2];
-        for (int round = 0; round < 2; ++round) {          // first the ties are numbered, then what leaves
-            const bool leaves = may && (key < prefix || (tie && round && (uint64_t)ties + all[0] < need));
-            scan[cur][threadIdx.x] = round ? leaves : tie;
-            __syncthreads();
-            for (int off = 1; off < kEvictBlock; off <<= 1) {
-                scan[cur ^ 1][threadIdx.x] = scan[cur][threadIdx.x] + ((int)threadIdx.x >= off ? scan[cur][threadIdx.x - off] : 0);
-                cur ^= 1;
-                __syncthreads();
-            }
-            const uint32_t incl = scan[cur][threadIdx.x], total = scan[cur][kEvictBlock - 1];
-            if (round == 0) {
-                all[0] = incl - tie;
-                all[1] = total;
-                __syncthreads();
-                continue;
-            }
-            const int64_t in_tile = min((int64_t)kEvictBlock, count - e0);
-            if (e < count) {
-                const int64_t from = first + e;
-                if (leaves) {
-                    const int64_t to = before + gone + incl - 1;
-                    if (to < a.list_capacity) {
-                        if (a.evict_ids) a.evict_ids[to] = a.ids[from];
-                        a.evict_slots[to] = a.slots[from];
-                    }
-                } else {
-                    const int64_t to = first + kept + threadIdx.x - incl;
-                    if (a.kept_weight) a.kept_weight[to] = w;
-                    if (a.kept_ids) a.kept_ids[to] = a.ids[from];
-                    a.kept_slots[to] = a.slots[from];
-                    if (a.kept_pos) a.kept_pos[to] = a.pos[from];
+}
+
+// ---- what stays and what leaves, of one wavefront's stretch ------------------------------------------------------------------
+// Ranks are popcounts of ballots; kAhead steps' loads are in flight together.
+constexpr int kAhead = 4;
+__device__ __forceinline__ void move_stretch(const EvictArgs& a, const Part& p, const Choice& c, int begin, int end, uint32_t tie, uint32_t gone) {
+    const int lane = threadIdx.x % 64;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    const bool over = p.count > a.budget;
+    const int may0 = a.sinks, may1 = p.count - a.recent;
+    for (int e0 = begin; e0 < end; e0 += 64 * kAhead) {
+        float w[kAhead];
+        int64_t id[kAhead];
+        int32_t slot[kAhead], pos[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int e = e0 + i * 64 + lane;
+            const int64_t from = p.first + e;
+            if (e >= end) continue;
+            w[i] = a.weight[from];
+            id[i] = a.ids ? a.ids[from] : 0;
+            slot[i] = a.slots[from];
+            pos[i] = a.pos ? a.pos[from] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int e = e0 + i * 64 + lane;
+            const bool in = e < end, may = over && in && e >= may0 && e < may1;
+            const uint32_t k = weight_key(w[i]);
+            const uint64_t ties = __ballot(may && k == c.key);
+            const bool leaves = may && (k < c.key || (k == c.key && tie + __popcll(ties & below) < c.ties));
+            const uint64_t leaving = __ballot(leaves);
+            const uint32_t left = gone + __popcll(leaving & below);        // entries of the list that leave before this one
+            if (leaves) {
+                const int64_t to = c.before + left;
+                if (to < a.list_capacity) {
+                    if (a.evict_ids) a.evict_ids[to] = id[i];
+                    a.evict_slots[to] = slot[i];
                 }
+            } else if (in) {
+                const int64_t to = p.first + e - left;
+                if (a.kept_weight) a.kept_weight[to] = w[i];
+                if (a.kept_ids) a.kept_ids[to] = id[i];
+                a.kept_slots[to] = slot[i];
+                if (a.kept_pos) a.kept_pos[to] = pos[i];
             }
-            gone += total;
-            kept += in_tile - total;
-            ties += all[1];
-            __syncthreads();
+            tie += __popcll(ties);
+            gone += __popcll(leaving);
         }
     }
+}
+
+// The evict lists behind the last entry, a share a workgroup.
+template <int BLOCK>
+__device__ __forceinline__ void clear_rest(const EvictArgs& a, int64_t all) {
+    for (int64_t e = all + (int64_t)blockIdx.x * BLOCK + threadIdx.x; e < a.list_capacity; e += (int64_t)gridDim.x * BLOCK) {
+        if (a.evict_ids) a.evict_ids[e] = -1;
+        a.evict_slots[e] = -1;
+    }
+}
+
+template <int BLOCK>
+struct Stretch {
+    int steps, begin, end;
+    __device__ __forceinline__ Stretch(const Part& p, int wave) {
+        const int places = p.end - p.begin;
+        steps = places / BLOCK + (places % BLOCK != 0);
+        begin = p.begin + (int)min((int64_t)places, (int64_t)wave * steps * 64);
+        end = (int)min((int64_t)p.end, (int64_t)begin + steps * 64);
+    }
+};
+
+// PASS 0: offsets, lengths, the evict lists' rest, and the first digit; lists of one part go on to the end.  PASS 1, 2: the next digits
+// of lists of several pieces; PASS 3: their ranks.  FUSED: entries are moved here too (lists of one part).
+template <int BLOCK, bool FUSED, int PASS>
+__global__ __launch_bounds__(BLOCK) void evict_select_kernel(EvictArgs a) {
+    constexpr int kHeld = BLOCK == 1024 ? 32 : 16, WAVES = BLOCK / 64, COPIES = BLOCK == 1024 ? 4 : 2, PER = kBins / BLOCK;
+    __shared__ uint32_t hist[COPIES][kBins + 1], found, rest, waves[WAVES];
+    __shared__ uint32_t counts[2][WAVES];
+    __shared__ int64_t sums[2][WAVES];
+    __shared__ uint64_t lows[2][WAVES];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const Part p = find_part(a, blockIdx.x);
+    if (PASS > 0 && (p.of == 1 || p.number >= p.of)) return;
+    const int over = max(0, p.count - a.budget);
+    const Stretch<BLOCK> mine(p, wave);
+    const bool held = mine.steps <= kHeld;
+    uint32_t key[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const int e = mine.begin + i * 64 + lane;
+        key[i] = over && held && e < mine.end ? weight_key(a.weight[p.first + e]) : 0;
+    }
+    Choice c{0, (uint32_t)over, 0};
+    if (PASS == 0) {
+        // what leaves the lists before this one, and all lists
+        int64_t before = 0, all = 0;
+        if (a.scanned) {
+            before = a.evict_off[min(p.bag, a.bags)];
+            all = a.evict_off[a.bags];
+        } else {
+            for (int64_t b = threadIdx.x; b < a.bags; b += BLOCK) {
+                int64_t f, n;
+                list_span(a, b, &f, &n);
+                const int64_t o = max(int64_t(0), n - a.budget);
+                all += o;
+                if (b < p.bag) before += o;
+            }
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) {
+                before += __shfl_xor(before, off);
+                all += __shfl_xor(all, off);
+            }
+            if (lane == 0) {
+                sums[0][wave] = before;
+                sums[1][wave] = all;
+            }
+            __syncthreads();
+            before = all = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                before += sums[0][w];
+                all += sums[1][w];
+            }
+            if (threadIdx.x == 0 && p.bag < a.bags && p.number == 0) a.evict_off[p.bag] = before;
+            if (threadIdx.x == 0 && blockIdx.x == 0) a.evict_off[a.bags] = all;
+        }
+        c.before = before;
+        if (threadIdx.x == 0 && p.bag < a.bags && p.number == 0) a.kept_len[p.bag] = (int32_t)(p.count - over);
+        if (FUSED) clear_rest<BLOCK>(a, all);
+        if (p.begin >= p.end) return;
+    } else {
+        c = a.choice[blockIdx.x];
+    }
+    const int may0 = a.sinks, may1 = p.count - a.recent;
+    // f(place, key) for the stretch, 64 places at a time; places past its end come as the list's length
+    const auto each = [&](auto&& f) {
+        if (held) {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (i < mine.steps) {
+                    const int e = mine.begin + i * 64 + lane;
+                    f(e < mine.end ? e : p.count, key[i]);
+                }
+        } else {
+            for (int e = mine.begin + lane; e - lane < mine.end; e += 64) f(e < mine.end ? e : p.count, e < mine.end ? weight_key(a.weight[p.first + e]) : 0u);
+        }
+    };
+    const auto count_digit = [&](int digit) {
+        for (int i = threadIdx.x; i < COPIES * (kBins + 1); i += BLOCK) (&hist[0][0])[i] = 0;
+        __syncthreads();
+        const int shift = kShift[digit], above = shift + kWidth[digit];
+        each([&](int e, uint32_t k) {
+            if (e >= may0 && e < may1 && (digit == 0 || (k ^ c.key) >> above == 0)) atomicAdd(&hist[lane % COPIES][k >> shift & ((1 << kWidth[digit]) - 1)], 1u);
+        });
+        __syncthreads();
+    };
+    const auto take_digit = [&](int digit, const uint32_t (&n)[PER]) {
+        find_digit<BLOCK>(n, c.ties, waves, &found, &rest);
+        __syncthreads();
+        c.key |= found << kShift[digit];
+        c.ties = rest;
+    };
+    uint32_t tie = 0, gone = 0;                       // of the list, before this part
+    if (over && p.of == 1 && over <= kFew) {          // one after the other: the lowest key, of those the earliest place
+        uint64_t last = 0;
+        c.ties = 0;
+        for (int round = 0; round < over; ++round) {
+            uint64_t low = ~uint64_t(0);
+            each([&](int e, uint32_t k) {
+                const uint64_t v = (uint64_t)k << 32 | (uint32_t)e;
+                if (e >= may0 && e < may1 && (round == 0 || v > last)) low = min(low, v);
+            });
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) low = min(low, (uint64_t)__shfl_xor(low, off));
+            if (lane == 0) lows[round % 2][wave] = low;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) low = min(low, lows[round % 2][w]);
+            c.ties = round > 0 && (uint32_t)(low >> 32) == (uint32_t)(last >> 32) ? c.ties + 1 : 1;
+            last = low;
+        }
+        c.key = (uint32_t)(last >> 32);
+    } else if (over && p.of == 1) {
+#pragma unroll
+        for (int digit = 0; digit < kDigits; ++digit) {
+            count_digit(digit);
+            uint32_t n[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                n[i] = 0;
+#pragma unroll
+                for (int k = 0; k < COPIES; ++k) n[i] += hist[k][PER * threadIdx.x + i];
+            }
+            take_digit(digit, n);
+        }
+    }
+    if (over && p.of > 1) {
+        if (PASS > 0) {                               // the digit that the pass before counted, over the list's pieces
+            uint32_t n[PER], mine_before = 0, all;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) n[i] = 0;
+            for (uint32_t q = 0; q < p.of; ++q) {
+                const uint32_t* const h = a.hist + ((int64_t)(p.first_id + q) * kDigits + PASS - 1) * kBins + PER * threadIdx.x;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) n[i] += h[i];
+            }
+            take_digit(PASS - 1, n);
+            if (PASS == kDigits) {                    // entries of the pieces before that have a lower key, or the same
+                for (uint32_t q = 0; q < p.number; ++q)
+#pragma unroll
+                    for (int d = 0; d < kDigits; ++d) {
+                        const uint32_t* const h = a.hist + ((int64_t)(p.first_id + q) * kDigits + d) * kBins;
+                        const uint32_t digit = c.key >> kShift[d] & ((1 << kWidth[d]) - 1);
+                        for (uint32_t i = threadIdx.x; i < digit; i += BLOCK) mine_before += h[i];
+                        if (d == kDigits - 1) tie += h[digit];
+                    }
+                __syncthreads();
+                sum_before<BLOCK>(mine_before, waves, &all);
+                gone = all;
+                __syncthreads();
+            }
+        }
+        if (PASS < kDigits) {
+            count_digit(PASS);
+            for (int i = threadIdx.x; i < kBins; i += BLOCK) {
+                uint32_t n = 0;
+#pragma unroll
+                for (int k = 0; k < COPIES; ++k) n += hist[k][i];
+                a.hist[((int64_t)blockIdx.x * kDigits + PASS) * kBins + i] = n;
+            }
+            if (threadIdx.x == 0) a.choice[blockIdx.x] = c;
+            return;
+        }
+    }
+    // ranks: ties before this wavefront, and what leaves before it
+    uint32_t n_tie = 0, n_less = 0;
+    if (over)
+        each([&](int e, uint32_t k) {
+            const bool may = e >= may0 && e < may1;
+            n_tie += __popcll(__ballot(may && k == c.key));
+            n_less += __popcll(__ballot(may && k < c.key));
+        });
+    if (lane == 0) {
+        counts[0][wave] = n_tie;
+        counts[1][wave] = n_less;
+    }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+        tie += counts[0][w];
+        gone += counts[1][w];
+    }
+    gone += min(tie, c.ties);
+    if (FUSED) {
+        move_stretch(a, p, c, mine.begin, mine.end, tie, gone);
+    } else {
+        if (lane == 0) a.begins[(int64_t)blockIdx.x * kStretches + wave] = make_uint2(tie, gone);
+        if (threadIdx.x == 0) a.choice[blockIdx.x] = c;
+    }
+}
+
+// A wavefront a stretch of 1,024 threads' selection.
+constexpr int kMoveBlock = 256;
+__global__ __launch_bounds__(kMoveBlock) void evict_move_kernel(EvictArgs a) {
+    const uint32_t job = blockIdx.x * (kMoveBlock / 64) + threadIdx.x / 64, part = job / kStretches;
+    const Part p = find_part(a, part);
+    const Stretch<1024> mine(p, job % kStretches);
+    clear_rest<kMoveBlock>(a, a.evict_off[a.bags]);
+    if (mine.begin >= mine.end) return;
+    const Choice c = a.choice[part];
+    const uint2 b = a.begins[job];
+    move_stretch(a, p, c, mine.begin, mine.end, b.x, b.y);
+}
+
+// Offsets of the evict lists where there are too many lists for every workgroup to add them up.
+__global__ __launch_bounds__(1024) void evict_scan_kernel(EvictArgs a) {
+    __shared__ int64_t sums[16];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    int64_t total = 0;
+    for (int64_t b0 = 0; b0 < a.bags; b0 += 1024) {
+        const int64_t b = b0 + threadIdx.x;
+        int64_t f, n = 0;
+        if (b < a.bags) list_span(a, b, &f, &n);
+        const int64_t o = max(int64_t(0), n - a.budget);
+        int64_t upto = o;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t x = __shfl_up(upto, off);
+            if (lane >= off) upto += x;
+        }
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        int64_t before = total + upto - o;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) before += sums[w];
+            total += sums[w];
+        }
+        if (b < a.bags) a.evict_off[b] = before;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) a.evict_off[a.bags] = total;
+}
+
+constexpr int64_t kManyLists = 4096;
+// Lists of up to 2,048 entries in the mean: 256 threads a list, one launch.  Longer ones: 1,024 threads choose, and a second launch
+// moves, 16 wavefronts a list wherever there is room.  From 16,384 on (a workgroup holds twice that) by pieces.
+bool lists_short(int64_t n, int64_t bags) { return n <= 2048 * std::max<int64_t>(bags, 1); }
+bool lists_long(int64_t n, int64_t bags) { return n > (kPiece / 2) * std::max<int64_t>(bags, 1) && n > kPiece; }
+
+struct EvictScratch {
+    Choice* choice;
+    uint2* begins;
+    uint32_t* hist;
+    size_t bytes;
+    EvictScratch(void* ws, int64_t n, int64_t bags) {
+        // room for any n and number of lists up to these
+        const int64_t pieces = (n >> kPieceShift) + std::min(bags, (n >> (kPieceShift - 1)) + 1), whole = std::min(bags, n / 2048 + 1);
+        Carver c(ws, 0);
+        choice = c.take<Choice>((size_t)std::max(pieces, whole));
+        begins = c.take<uint2>((size_t)std::max(pieces, whole) * kStretches);
+        hist = c.take<uint32_t>(n > kPiece ? (size_t)pieces * kDigits * kBins : 0);
+        bytes = c.used();
+    }
+};
+
+int launch_evict(EvictArgs a, hipStream_t stream) {
+    a.scanned = a.bags > kManyLists;
+    if (a.scanned) BP_LAUNCH(K_EVICT_SELECT, evict_scan_kernel, dim3(1), dim3(1024), 0, stream, a);
+    a.split = lists_long(a.n, a.bags);
+    a.parts = (uint32_t)(a.split ? (a.n >> kPieceShift) + a.bags : a.bags);
+    const unsigned parts = std::max(a.parts, 1u);
+    // enough workgroups for the evict lists' rest, too
+    const auto grid = [&](int64_t groups, int block) { return dim3((unsigned)std::max(groups, std::min<int64_t>(ceil_div(a.list_capacity, 8 * block), 1024))); };
+    if (lists_short(a.n, a.bags)) {
+        BP_LAUNCH(K_EVICT_SELECT, (evict_select_kernel<256, true, 0>), grid(parts, 256), dim3(256), 0, stream, a);
+        return BP_OK;
+    }
+    BP_LAUNCH(K_EVICT_SELECT, (evict_select_kernel<1024, false, 0>), dim3(parts), dim3(1024), 0, stream, a);
+    if (a.split) {
+        BP_LAUNCH(K_EVICT_SELECT, (evict_select_kernel<1024, false, 1>), dim3(a.parts), dim3(1024), 0, stream, a);
+        BP_LAUNCH(K_EVICT_SELECT, (evict_select_kernel<1024, false, 2>), dim3(a.parts), dim3(1024), 0, stream, a);
+        BP_LAUNCH(K_EVICT_SELECT, (evict_select_kernel<1024, false, 3>), dim3(a.parts), dim3(1024), 0, stream, a);
+    }
+    BP_LAUNCH(K_EVICT_MOVE, evict_move_kernel, grid(ceil_div((int64_t)parts * kStretches, kMoveBlock / 64), kMoveBlock), dim3(kMoveBlock), 0, stream, a);
+    return BP_OK;
 }
 
 }  // namespace
@@ -171,7 +517,7 @@ BP_EXPORT int bp_evict_by_weight_workspace_bytes(int64_t n, int64_t bags, size_t
     if (!bytes) return fail(BP_ERR_INVALID_ARG, "bytes is NULL");
     if (n < 0 || bags < 0) return fail(BP_ERR_INVALID_ARG, "negative size");
     if (n >= (int64_t(1) << 31) || bags >= kMaxLists) return fail(BP_ERR_UNSUPPORTED, "n >= 2^31 or bags >= 2^24");
-    *bytes = 0;
+    *bytes = EvictScratch(nullptr, n, bags).bytes;
     return BP_OK;
 }
 
@@ -203,8 +549,11 @@ BP_EXPORT int bp_evict_by_weight(const int64_t* bag_offsets, const int32_t* bag_
             if (from[i] && to[j] && (uintptr_t)from[i] < (uintptr_t)to[j] + n * wide[j] && (uintptr_t)to[j] < (uintptr_t)from[i] + n * wide[i])
                 return fail(BP_ERR_INVALID_ARG, "the kept arrays overlap the input arrays");
     if (bags && kept_lengths == bag_lengths) return fail(BP_ERR_INVALID_ARG, "kept_lengths is bag_lengths");
-    const EvictArgs a{bag_offsets, bag_lengths, n, bags, budget, sinks, recent, weight, ids, slots, pos, kept_weight, kept_ids, kept_slots,
-                      kept_pos, kept_lengths, evict_ids, evict_slots, list_capacity, evict_offsets};
-    BP_LAUNCH(K_EVICT_SELECT, evict_kernel, dim3((unsigned)std::max<int64_t>(bags, 1)), dim3(kEvictBlock), 0, (hipStream_t)stream, a);
-    return BP_OK;
+    if (need && (!workspace || ((uintptr_t)workspace & 255))) return fail(BP_ERR_INVALID_ARG, "workspace NULL or not 256-byte aligned");
+    if (workspace_bytes < need) return fail(BP_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < required %zu bytes", workspace_bytes, need);
+    const EvictScratch w(workspace, n, bags);
+    return launch_evict(EvictArgs{bag_offsets, bag_lengths, n, bags, budget, sinks, recent, weight, ids, slots, pos, kept_weight, kept_ids,
+                                  kept_slots, kept_pos, kept_lengths, evict_ids, evict_slots, list_capacity, evict_offsets, 0, 0, 0, w.choice,
+                                  w.begins, w.hist},
+                        (hipStream_t)stream);
 }
