@@ -83,7 +83,7 @@ const char* const kKernelNames[K_NUM_KERNELS] = {
     "plan_keys", "plan_pairs", "plan_hist", "plan_occupancy", "plan_flags", "plan_lists", "plan_ring_jump",
     "plan_slots", "plan_group", "cache_evict", "cache_prefetch", "cache_stage", "cache_duplex", "embbag_fwd", "bwd_keys", "bwd_items", "bwd_reduce_update",
     "fill", "copy_calibration", "relpos_bias_fwd", "relpos_bias_bwd", "relpos_bias_join", "relpos_update", "embbag_attn_fwd",
-    "embbag_attn_bwd", "embbag_attn_join", "evict_select", "evict_move"};
+    "embbag_attn_bwd", "embbag_attn_join", "embbag_attn_weight", "evict_select", "evict_move"};
 }  // namespace
 
 bool profile_events(int id, hipEvent_t* start, hipEvent_t* stop) {

@@ -54,41 +54,70 @@ __device__ __forceinline__ BagSpan bag_span(const AttnArgs& a, int64_t bag) {
 __device__ __forceinline__ float row_value(const float* row, int64_t i) { return row[i]; }
 __device__ __forceinline__ float row_value(const uint16_t* row, int64_t i) { return bf16_bits_to_f32(row[i]); }
 
-// Bags are handed out in pieces of 1 << shift entries.  Piece numbers need no scan over the bags: bag b's begin at
-// (its offset >> shift) + b, which leaves every bag room for all its pieces (and some numbers without one).
-__device__ __forceinline__ uint32_t first_piece(const AttnArgs& a, int shift, uint32_t bag) {
+// Bags are handed out in pieces of 1 << shift entries, numbered without a scan over the bags: numbers below `bags` are the bags'
+// first pieces; the others of bag b begin at bags + (its offset >> shift), which leaves every bag room for all of its pieces (and
+// some numbers without one).
+inline int64_t piece_count(int64_t n, int64_t bags, int shift) { return (n >> shift) + bags; }
+__device__ __forceinline__ uint32_t more_pieces(const AttnArgs& a, int shift, uint32_t bag) {
     int64_t at = a.bag_off[bag];
     if (at < 0) at = 0;
     if (at > a.n) at = a.n;
-    return (uint32_t)(at >> shift) + bag;
+    return (uint32_t)(at >> shift);
 }
-inline int64_t piece_count(int64_t n, int64_t bags, int shift) { return (n >> shift) + bags; }
 
 struct BagPiece {
-    uint32_t bag, number, of;         // piece `number` of the bag's `of` (0 for an empty bag, which has the piece 0 all the same)
-    uint32_t first_id;                // the number of the bag's first piece among all
+    uint32_t bag, number, of;         // piece `number` of the bag's `of` (at least 1); a number without a piece has number >= of
+    uint32_t more;                    // the bag's pieces 1, 2, ... have the numbers more, more + 1, ...
     int64_t first;                    // its entries
     int count;
 };
-// The piece with number `id` among `all`: the last bag that begins no later, found 64 bags a step by every wavefront.
-__device__ __forceinline__ BagPiece find_piece(const AttnArgs& a, int shift, uint32_t id, uint32_t all) {
-    const uint32_t lane = threadIdx.x % 64;
+__device__ __forceinline__ uint32_t piece_id(const BagPiece& p, uint32_t number) { return number == 0 ? p.bag : p.more + number - 1; }
+__device__ __forceinline__ BagPiece bag_piece(const AttnArgs& a, int shift, uint32_t bag, uint32_t number, const BagSpan& s) {
+    BagPiece p;
+    const uint32_t at = more_pieces(a, shift, bag), extra = (uint32_t)(a.n >> shift);
+    p.bag = bag;
+    p.number = number;
+    p.more = (uint32_t)a.bags + at;
+    p.of = max(1u, min((uint32_t)((s.count + (1 << shift) - 1) >> shift), 1 + extra - at));
+    p.first = s.first + ((int64_t)number << shift);
+    p.count = number < p.of ? (int)min(int64_t(1) << shift, s.count - ((int64_t)number << shift)) : 0;
+    return p;
+}
+// A multiplier that spreads 0 .. count - 1 over themselves (count and it have no common factor).
+inline uint32_t spread_of(int64_t count) {
+    if (count < 3) return 1;
+    uint64_t k = (uint64_t)(0.6180339887 * (double)count) | 1;
+    const auto common = [](uint64_t a, uint64_t b) {
+        while (b) {
+            const uint64_t t = a % b;
+            a = b;
+            b = t;
+        }
+        return a;
+    };
+    while (common(k, (uint64_t)count) != 1) ++k;
+    return (uint32_t)(k % (uint64_t)count);
+}
+
+// Workgroup w's piece number.  Bags with room to grow have real pieces first and then numbers without one, at distances that tend
+// to be powers of two; taken in order, some of the chip's eight dies, to which workgroups are dealt in turn, get most of the real
+// ones (64 lists of up to 8,192 entries in stretches of 8,192: 117 us in order, 87 spread).
+__device__ __forceinline__ uint32_t spread_piece(const AttnArgs& a, int shift, uint32_t spread, uint32_t w) {
+    if (w < (uint32_t)a.bags) return w;
+    return (uint32_t)a.bags + (uint32_t)((uint64_t)(w - (uint32_t)a.bags) * spread % (uint64_t)(a.n >> shift));
+}
+
+// The piece with number `id`; behind the first pieces the bag is looked for, 64 bags a step by every wavefront.
+__device__ __forceinline__ BagPiece find_piece(const AttnArgs& a, int shift, uint32_t id) {
+    if (id < (uint32_t)a.bags) return bag_piece(a, shift, id, 0, bag_span(a, id));
+    const uint32_t lane = threadIdx.x % 64, x = id - (uint32_t)a.bags;
     uint32_t lo = 0, hi = (uint32_t)a.bags;
-    while (hi - lo > 1) {
+    while (hi - lo > 1) {             // the last bag whose numbers begin no later
         const uint32_t step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step;
-        const bool starts = i < hi && first_piece(a, shift, i) <= id;
-        lo += __popcll(__ballot(starts)) * step;
+        lo += __popcll(__ballot(i < hi && more_pieces(a, shift, i) <= x)) * step;
         hi = min(hi, lo + step);
     }
-    const BagSpan s = bag_span(a, lo);
-    BagPiece p;
-    p.bag = lo;
-    p.first_id = first_piece(a, shift, lo);
-    p.number = id - p.first_id;
-    p.of = min((uint32_t)((s.count + (1 << shift) - 1) >> shift), all - min(all, p.first_id));
-    p.first = s.first + ((int64_t)p.number << shift);
-    p.count = p.number < p.of ? (int)min(int64_t(1) << shift, s.count - ((int64_t)p.number << shift)) : 0;
-    return p;
+    return bag_piece(a, shift, lo, x - more_pieces(a, shift, lo) + 1, bag_span(a, lo));
 }
 
 // exp of a difference: scores stay in natural units up to here, so that the lowest fp32 value, which masks give, does not become

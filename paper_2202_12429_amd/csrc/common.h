@@ -128,6 +128,7 @@ enum KernelId {
     K_ATTN_FWD,
     K_ATTN_BWD,
     K_ATTN_JOIN,
+    K_ATTN_WEIGHT,
     K_EVICT_SELECT,
     K_EVICT_MOVE,
     K_NUM_KERNELS

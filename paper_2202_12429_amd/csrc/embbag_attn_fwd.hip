@@ -91,11 +91,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 struct FwdArgs {
     AttnArgs a;
     int32_t shift;              // log2 of a piece's entries
-    int32_t heads;              // kv heads of a workgroup: 1, 2 or 4 of its four wavefronts' worth
-    uint32_t pieces;
-    float* scores;              // [n][q_heads]; NULL when no weights are asked for
-    float* part_ml;             // [pieces][q_heads][2]: maximum and sum of a piece
-    float* part_o;              // [pieces][q_heads][d]: its weighted values, not divided by the sum
+    uint32_t pieces, spread;
+    uint32_t groups;            // workgroups that share all entries evenly; 0: a workgroup a piece
+    uint32_t* blocks;           // [bags + 1] running count of the bags' blocks, written by the first of these workgroups
+    int32_t weighed;            // bags of one piece have their weights from the first launch
+    float* scores;              // [q_heads][score_stride]; NULL when no weights are asked for
+    int64_t score_stride;
+    float* part_ml;             // [parts][q_heads][2]: maximum and sum of a part of a bag
+    float* part_o;              // [parts][q_heads][d]: its weighted values, not divided by the sum
     float* out;
     float* lse;
     const float* weight_in;
@@ -103,7 +106,6 @@ struct FwdArgs {
 };
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kFwdBlock = 256, kFwdWaves = kFwdBlock / 64;
 
 // Three bf16 parts of an fp32 value whose sum it is exactly: the leading eight bits of what the parts before leave.
 __device__ __forceinline__ float leading(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
@@ -129,22 +131,43 @@ struct Split3 {
     }
 };
 
-// How a wavefront takes a tile of rows with the matrix instructions (rows down, the group's query heads across, of which it has
-// up to 16).  DP: head_dim rounded up.  Scores: S[row][head] = K Q^T, a lane loads 16 bytes of a row and its neighbours 16 rows
-// away the next 16.  Pooling: O^T[d][head] = V^T P^T; a row of S that a lane holds is an entry whose p that lane is asked for, so
-// p never leaves its lane, and V comes in whole rows: a lane loads VW elements, which serve VW products of 16 dims each.
+// How a wavefront takes a tile of rows with the matrix instructions: the rows' entries down, query heads across, of which there
+// are up to 16 columns: the groups of PACK kv heads, so that what is done with a score is done for all of them at once.
+// Scores: S[entry][column] = K Q^T for every kv head, of which a column takes its own head's; a lane loads 16 bytes of a row and
+// its neighbours 16 lanes away the next 16.  (A product of all heads' keys with a query padded by zeros would do without the
+// choice, but a NaN of one head would be another's too.)  Pooling: O^T[element][column] = V^T P^T over the heads' values side by
+// side, of which a column's own are taken at the end; an entry whose scores a lane holds is one whose p that lane is asked for,
+// so p never leaves its lane, and V comes in whole rows: a lane loads VW elements, which serve VW products of 16 elements each.
 // bf16 rows go through the bf16 instruction: q and p are cut into three bf16 parts, whose products are exact in fp32, so that
-// what is computed is fp32 (and the instruction's adder is idle for most of the time anyway: 8 TB/s of rows need a sixth of it).
-template <typename T, int DP>
+// what is computed is fp32.  DP: head_dim rounded up.
+template <typename T, int DP, int PACK>
 struct AttnTile {
     static constexpr bool BF16 = sizeof(T) == 2;
     static constexpr int ROWS = BF16 ? 32 : 16;        // entries of a tile
     static constexpr int NU = ROWS / 16;               // S tiles
     static constexpr int PER = ROWS / 4;               // entries a lane holds scores of
     static constexpr int KC = BF16 ? 32 : 16, KM = (DP + KC - 1) / KC;
-    static constexpr int VW = DP / 16 < (BF16 ? 8 : 4) ? DP / 16 : BF16 ? 8 : 4, MB = DP / (16 * VW);
+    static constexpr int FLAT = PACK * DP;             // elements of the heads' values
+    static constexpr int VW = FLAT / 16 < (BF16 ? 8 : 4) ? FLAT / 16 : BF16 ? 8 : 4, MB = FLAT / (16 * VW);
     static constexpr int OREGS = MB * VW * 4;
 };
+
+// weight_out of a piece's entries, a thread each, from the scores and the bag's norms.  A bag without one (nothing seen) has scores
+// of -infinity alone.
+template <int BLOCK>
+__device__ __forceinline__ void add_weights(const FwdArgs& f, uint32_t bag, int64_t first, int count) {
+    const float* const lse = f.lse + (int64_t)bag * f.a.q_heads;
+    for (int i = threadIdx.x; i < count; i += BLOCK) {
+        const int64_t k = first + i;
+        float add = 0.f;
+#pragma unroll 4
+        for (int h = 0; h < f.a.q_heads; ++h) {
+            const float c = f.scores[h * f.score_stride + k];
+            add += c == -INFINITY ? 0.f : exp_few_ulp(c - lse[h]);
+        }
+        f.weight_out[k] = (f.weight_in ? f.weight_in[k] : 0.f) + add;
+    }
+}
 
 template <int BYTES>
 struct Bytes {
@@ -159,41 +182,65 @@ __device__ __forceinline__ uint32_t masked(uint32_t v, uint32_t m) { return v & 
 
 // LDS of a workgroup, in this order: borders, every wavefront's slots and table rows of a tile, its maxima and sums, the bias
 // table's columns of the workgroup's heads, and (over the table, once it is done with) the wavefronts' weighted values.
-constexpr int kLdsBorders = 0, kLdsTile = BP_RELPOS_MAX_BUCKETS, kLdsMl = kLdsTile + kFwdWaves * 64, kLdsFree = kLdsMl + kFwdWaves * 32;
-inline size_t attn_fwd_lds(int dp, int table_floats) {
-    return (size_t)(kLdsFree + std::max(table_floats, kFwdWaves * (dp / 4) * 65)) * 4;
-}
+template <int WAVES>
+struct AttnLds {
+    static constexpr int BORDERS = 0, TILE = BP_RELPOS_MAX_BUCKETS, ML = TILE + WAVES * 128, FREE = ML + WAVES * 32;
+    static size_t bytes(int flat, int table_floats) { return (size_t)(FREE + std::max(table_floats, WAVES * (flat / 4) * 64)) * 4; }
+};
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kFwdBlock) void embbag_attn_fwd_kernel(FwdArgs f) {
-    typedef AttnTile<T, DP> X;
+// Entries [first, first + count) of a bag: all that it uses, or the part with this number.
+struct Segment {
+    uint32_t bag, part;
+    int64_t first;
+    int count;
+    bool whole;
+};
+
+constexpr int kFwdWaves = 4, kFwdBlock = kFwdWaves * 64;
+template <typename T, int DP, int PACK>
+__device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float* lds) {
+    typedef AttnLds<kFwdWaves> L;
+    constexpr int kLdsBorders = L::BORDERS, kLdsTile = L::TILE, kLdsMl = L::ML, kLdsFree = L::FREE;
+    typedef AttnTile<T, DP, PACK> X;
     typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
-    extern __shared__ float lds[];
     const AttnArgs& a = f.a;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
-    const BagPiece p = find_piece(a, f.shift, blockIdx.x, f.pieces);
-    if (p.number > 0 && p.number >= p.of) return;
-    const int group = a.q_heads / a.kv_heads, heads = f.heads, stripes = kFwdWaves / heads;
-    const int kv0 = blockIdx.y * heads, kv = kv0 + wave % heads, stripe = wave / heads;
-    const int first_head = kv0 * group, table_cols = heads * group;
+    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = min(PACK, a.kv_heads - kv0);
+    constexpr int stripes = kFwdWaves;
+    const int stripe = wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * a.d;
+    const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;        // the column's query head, its kv head
 
     int32_t* const borders = (int32_t*)lds + kLdsBorders;
-    int32_t* const tile = (int32_t*)lds + kLdsTile + wave * 64;
+    int32_t* const tiles_of = (int32_t*)lds + kLdsTile + wave * 128;          // two tiles: slots, table offsets
     float* const table = lds + kLdsFree;
+
+    // entry `lane` of a tile: its slot and position, fetched ahead
+    const int tiles = (p.count + X::ROWS - 1) / X::ROWS;
+    int32_t slot_n = -1, pos_n = 0;
+    const auto fetch = [&](int t) {
+        const int e = t * X::ROWS + lane;
+        const bool have = lane < X::ROWS && e < p.count;
+        slot_n = have ? a.slots[p.first + e] : -1;
+        pos_n = have && a.bias ? a.lookup_pos[p.first + e] : 0;
+    };
+    fetch(stripe);
+    const int64_t q_pos = a.bias ? a.q_pos[p.bag] : 0;
     if (a.bias) {
         if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = a.rp.borders[threadIdx.x];
-        for (int e = threadIdx.x; e < a.rp.rows() * table_cols; e += kFwdBlock)
-            table[e] = a.bias[(e / table_cols) * a.q_heads + first_head + e % table_cols];
+        if (table_cols == a.q_heads)
+            for (int e = threadIdx.x; e < a.rp.rows() * table_cols; e += kFwdBlock) table[e] = a.bias[e];
+        else
+            for (int e = threadIdx.x; e < a.rp.rows() * table_cols; e += kFwdBlock)
+                table[e] = a.bias[(e / table_cols) * a.q_heads + first_head + e % table_cols];
     }
 
-    // the group's queries: lane col has query head col
-    const int head = kv * group + min(col, group - 1);
+    // the queries: lane col has the column's
     const float* const q = a.q + ((int64_t)p.bag * a.q_heads + head) * a.d;
     std::conditional_t<X::BF16, Split3, f32x4> qf[X::KM];
 #pragma unroll
     for (int m = 0; m < X::KM; ++m) {
         const int at = m * X::KC + g * (X::KC / 4);
-        const bool have = col < group && at < a.d;
+        const bool have = col < cols && at < a.d;
         if constexpr (X::BF16) {
             float v[8];
 #pragma unroll
@@ -207,8 +254,7 @@ __global__ __launch_bounds__(kFwdBlock) void embbag_attn_fwd_kernel(FwdArgs f) {
             qf[m] = f32x4{t.x, t.y, t.z, t.w};
         }
     }
-    const int64_t q_pos = a.bias ? a.q_pos[p.bag] : 0;
-    __syncthreads();
+    if (a.bias) __syncthreads();
 
     f32x4 o[X::MB][X::VW];
 #pragma unroll
@@ -216,86 +262,114 @@ __global__ __launch_bounds__(kFwdBlock) void embbag_attn_fwd_kernel(FwdArgs f) {
 #pragma unroll
         for (int j = 0; j < X::VW; ++j) o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, sum = 0.f;             // of the lane's query head; the sum over the lane's own entries
-    const T* const w = (const T*)a.cache_w + (int64_t)kv * a.d;
-    const int tiles = (p.count + X::ROWS - 1) / X::ROWS;
+    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * a.d;
 
-    // entry `lane` of the tile: its slot and position, one tile ahead
-    int32_t slot_n = -1, pos_n = 0;
-    const auto fetch = [&](int t) {
-        const int e = t * X::ROWS + lane;
-        const bool have = lane < X::ROWS && e < p.count;
-        slot_n = have ? a.slots[p.first + e] : -1;
-        pos_n = have && a.bias ? a.lookup_pos[p.first + e] : 0;
-    };
-    fetch(stripe);
-    for (int t = stripe; t < tiles; t += stripes) {
+    // What a tile takes, a step ahead of its use: slots and table offsets into LDS, keys as soon as the tile before has its scores,
+    // values as soon as it has pooled, so that one or the other is always on its way, in the registers that it falls free of.
+    bool all_seen_n = true;
+    const auto place = [&](int t) {               // what fetch() brought, for tile t
         int row_of = -1;
         if ((uint32_t)slot_n < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - pos_n, borders, a.rp.buckets, a.rp.two_sided) : 0;
-        const bool all_seen = __ballot(row_of >= 0 || lane >= X::ROWS) == ~0ull;
+        all_seen_n = __ballot(row_of >= 0 || lane >= X::ROWS) == ~0ull;
+        int32_t* const tile = tiles_of + (t / stripes & 1) * 64;
+        __builtin_amdgcn_wave_barrier();
         if (lane < X::ROWS) {
             tile[lane] = row_of >= 0 ? slot_n : 0;                    // what is not seen reads row 0, and leaves it out
-            tile[32 + lane] = row_of;
+            tile[32 + lane] = row_of >= 0 ? row_of * table_cols : -1;
         }
-        fetch(t + stripes);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        // row `col` of S tile u is entry PER * (col / 4) + 4u + col % 4, so that lane (col, g)'s scores are of the entries PER * g ...
-        uint4 kraw[X::NU][X::KM];
+    };
+    // row `col` of S tile u is entry PER * (col / 4) + 4u + col % 4, so that lane (col, g)'s scores are of the entries PER * g ...
+    uint4 kraw[PACK][X::NU][X::KM];
+    const auto load_keys = [&](int t) {
+        const int32_t* const tile = tiles_of + (t / stripes & 1) * 64;
 #pragma unroll
         for (int u = 0; u < X::NU; ++u) {
             const T* const row = w + (int64_t)tile[X::PER * (col / 4) + 4 * u + col % 4] * a.wst;
 #pragma unroll
-            for (int m = 0; m < X::KM; ++m) {
-                const int at = m * X::KC + g * (X::KC / 4);
-                kraw[u][m] = at < a.d ? *reinterpret_cast<const uint4*>(row + at) : make_uint4(0, 0, 0, 0);
-            }
+            for (int k = 0; k < PACK; ++k)
+#pragma unroll
+                for (int m = 0; m < X::KM; ++m) {
+                    const int at = m * X::KC + g * (X::KC / 4);
+                    kraw[k][u][m] = at < a.d && k < heads ? *reinterpret_cast<const uint4*>(row + k * a.d + at) : make_uint4(0, 0, 0, 0);
+                }
         }
-        VRaw vraw[X::PER][X::MB];
-        int32_t row_t[X::PER];
+    };
+    VRaw vraw[X::PER][X::MB];
+    const auto load_values = [&](int t) {
+        const int32_t* const tile = tiles_of + (t / stripes & 1) * 64;
 #pragma unroll
         for (int e = 0; e < X::PER; ++e) {
             const T* const row = w + (int64_t)tile[X::PER * g + e] * a.wst + a.value_at;
-            row_t[e] = tile[32 + X::PER * g + e];
 #pragma unroll
             for (int m = 0; m < X::MB; ++m) {
                 const int at = m * 16 * X::VW + col * X::VW;
-                vraw[e][m] = *reinterpret_cast<const VRaw*>(row + (at < a.d ? at : 0));
+                vraw[e][m] = *reinterpret_cast<const VRaw*>(row + (at < flat ? at : 0));
             }
+        }
+    };
+    const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
+    const float* const column = table + min(col, cols - 1);
+    if (stripe < tiles) {
+        place(stripe);
+        load_keys(stripe);
+        load_values(stripe);
+        fetch(stripe + stripes);
+    }
+    for (int t = stripe; t < tiles; t += stripes) {
+        const bool all_seen = all_seen_n, more = t + stripes < tiles;
+        const int32_t* const tile = tiles_of + (t / stripes & 1) * 64;
+        if (more) {
+            place(t + stripes);
+            fetch(t + 2 * stripes);
         }
         float z[X::PER];
 #pragma unroll
         for (int u = 0; u < X::NU; ++u) {
-            f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int m = 0; m < X::KM; ++m) {
-                if constexpr (X::BF16) {
-                    const bf16x8 k = __builtin_bit_cast(bf16x8, kraw[u][m]);
+            for (int k = 0; k < PACK; ++k) {
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int part = 2; part >= 0; --part) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[m].part[part], s, 0, 0, 0);
-                } else {
+                for (int m = 0; m < X::KM; ++m) {
+                    if constexpr (X::BF16) {
+                        const bf16x8 key = __builtin_bit_cast(bf16x8, kraw[k][u][m]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kraw[u][m], e)), qf[m][e], s, 0, 0, 0);
+                        for (int part = 2; part >= 0; --part) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, qf[m].part[part], s, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kraw[k][u][m], e)), qf[m][e], s, 0, 0, 0);
+                    }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i];
+                for (int i = 0; i < 4; ++i) z[4 * u + i] = k == 0 || own == k ? s[i] : z[4 * u + i];
+            }
         }
+        if (more) load_keys(t + stripes);
+        int32_t row_t[X::PER];
+#pragma unroll
+        for (int e = 0; e < X::PER; ++e) row_t[e] = tile[32 + X::PER * g + e];
         float most = -INFINITY;
 #pragma unroll
         for (int e = 0; e < X::PER; ++e) {
-            float c = z[e] * a.scale;
-            if (a.cap > 0) c = a.cap * tanh_few_ulp(c / a.cap);
-            if (a.bias) c += table[max(row_t[e], 0) * table_cols + (wave % heads) * group + min(col, group - 1)];
+            float c = a.cap > 0 ? a.cap * tanh_few_ulp(z[e] * by_cap) : z[e] * a.scale;
+            if (a.bias) c += column[max(row_t[e], 0)];
             z[e] = row_t[e] >= 0 ? c : -INFINITY;
             most = fmaxf(most, z[e]);
         }
-        if (f.scores && col < group) {
+        if (f.scores && col < cols) {
+            const int e0 = t * X::ROWS + X::PER * g;
+            float* const to = f.scores + head * f.score_stride + p.first + e0;
+            if (e0 + X::PER <= p.count) {
 #pragma unroll
-            for (int e = 0; e < X::PER; ++e)
-                if (t * X::ROWS + X::PER * g + e < p.count)
-                    f.scores[(p.first + t * X::ROWS + X::PER * g + e) * a.q_heads + head] = z[e];
+                for (int e = 0; e < X::PER; e += 4) __builtin_memcpy(to + e, z + e, 16);        // aligned to a float
+            } else {
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e)
+                    if (e0 + e < p.count) to[e] = z[e];
+            }
         }
         // The reference of the exponentials moves only when a score exceeds it by more than 7 (a factor of 1,100, nothing to fp32).
         if (__ballot(most > top + 7.f || (top == -INFINITY && most > top))) {
@@ -347,14 +421,15 @@ __global__ __launch_bounds__(kFwdBlock) void embbag_attn_fwd_kernel(FwdArgs f) {
                     for (int j = 0; j < X::VW; ++j)
                         o[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vraw[e][m], j)), pr[e], o[m][j], 0, 0, 0);
         }
+        if (more) load_values(t + stripes);
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
 
-    // the wavefronts of a head meet
+    // the wavefronts meet: every lane leaves its sums, and takes up a fourth of the lane's own place of all four
     float* const ml = lds + kLdsMl;
     float* const ox = lds + kLdsFree;
-    constexpr int kWaveO = X::OREGS * 65;
+    constexpr int kWaveO = X::OREGS * 64;
     __syncthreads();                                                 // done with the table
     if (g == 0) {
         ml[wave * 32 + col] = top;
@@ -365,134 +440,284 @@ __global__ __launch_bounds__(kFwdBlock) void embbag_attn_fwd_kernel(FwdArgs f) {
 #pragma unroll
         for (int j = 0; j < X::VW; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ox[wave * kWaveO + ((m * X::VW + j) * 4 + i) * 65 + lane] = o[m][j][i];
+            for (int i = 0; i < 4; ++i) ox[wave * kWaveO + ((m * X::VW + j) * 4 + i) * 64 + lane] = o[m][j][i];
     __syncthreads();
-    const bool whole = p.of <= 1;
-    for (int e = threadIdx.x; e < heads * group * a.d; e += kFwdBlock) {
-        const int at = e % a.d, qh = e / a.d, c = qh % group, wh = qh / group;
-        const int row = at % (16 * X::VW) / X::VW, reg = (at / (16 * X::VW) * X::VW + at % X::VW) * 4 + row % 4, from = row / 4 * 16 + c;
-        float best = -INFINITY;
-        for (int s = 0; s < stripes; ++s) best = fmaxf(best, ml[(wh + s * heads) * 32 + c]);
-        const float ref = best == -INFINITY ? 0.f : best;
-        float l = 0.f, v = 0.f;
-        for (int s = 0; s < stripes; ++s) {
-            const int x = wh + s * heads;
-            const float k = exp_few_ulp(ml[x * 32 + c] - ref);
-            l = fmaf(k, ml[x * 32 + 16 + c], l);
-            v = fmaf(k, ox[x * kWaveO + reg * 65 + from], v);
-        }
-        const int h = first_head + qh;
-        if (whole) {
-            f.out[((int64_t)p.bag * a.q_heads + h) * a.d + at] = l == 0.f ? 0.f : v / l;
-            if (at == 0) f.lse[(int64_t)p.bag * a.q_heads + h] = l == 0.f ? -INFINITY : best + __builtin_amdgcn_logf(l) * kLn2;
+    float best = -INFINITY, l = 0.f, k[kFwdWaves];
+#pragma unroll
+    for (int x = 0; x < kFwdWaves; ++x) best = fmaxf(best, ml[x * 32 + col]);
+#pragma unroll
+    for (int x = 0; x < kFwdWaves; ++x) {
+        k[x] = exp_few_ulp(ml[x * 32 + col] - (best == -INFINITY ? 0.f : best));
+        l = fmaf(k[x], ml[x * 32 + 16 + col], l);
+    }
+    if (p.whole) {
+        const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int x = 0; x < kFwdWaves; ++x) k[x] = l == 0.f ? 0.f : k[x] * by;
+    }
+    if (wave == 0 && g == 0 && col < cols) {
+        if (p.whole) {
+            f.lse[(int64_t)p.bag * a.q_heads + head] = l == 0.f ? -INFINITY : best + __builtin_amdgcn_logf(l) * kLn2;
         } else {
-            f.part_o[((int64_t)blockIdx.x * a.q_heads + h) * a.d + at] = v;
-        }
-        if (at == 0 && (!whole || f.scores)) {
-            f.part_ml[((int64_t)blockIdx.x * a.q_heads + h) * 2] = best;
-            f.part_ml[((int64_t)blockIdx.x * a.q_heads + h) * 2 + 1] = l;
+            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2] = best;
+            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2 + 1] = l;
         }
     }
+    // VW elements of the column's head that lie side by side
+    float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * a.d : f.part_o + ((int64_t)p.part * a.q_heads + head) * a.d) - own * a.d;
+#pragma unroll
+    for (int m = 0; m < X::MB; ++m) {
+        const int at = (m * 16 + 4 * g + wave) * X::VW;
+        float v[X::VW];
+#pragma unroll
+        for (int j = 0; j < X::VW; ++j) {
+            v[j] = 0.f;
+#pragma unroll
+            for (int x = 0; x < kFwdWaves; ++x) v[j] = fmaf(k[x], ox[x * kWaveO + ((m * X::VW + j) * 4 + wave) * 64 + lane], v[j]);
+        }
+        if (col < cols && at >= own * a.d && at < (own + 1) * a.d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+    }
+    __syncthreads();                                                 // LDS is free again, the bag's lse there
 }
 
-// A workgroup a piece again: the bag's maxima and sums over its pieces, then this piece's share of the pooled rows and its own
-// entries' weights.
-constexpr int kShare = 16;                        // elements of the pooled rows that a workgroup sums at a time, 64 bytes
-__global__ __launch_bounds__(kFwdBlock) void embbag_attn_join_kernel(FwdArgs f) {
+// A workgroup a piece: calls whose bags are short, or so many that they even out.
+template <typename T, int DP, int PACK>
+__global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_fwd_kernel(FwdArgs f) {
     extern __shared__ float lds[];
+    const uint32_t id = spread_piece(f.a, f.shift, f.spread, blockIdx.x);
+    const BagPiece p = find_piece(f.a, f.shift, id);
+    if (p.number >= p.of) return;
+    attend<T, DP, PACK>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
+    if (f.scores && p.of == 1 && f.weighed) add_weights<kFwdBlock>(f, p.bag, p.first, p.count);       // all heads were this workgroup's
+}
+
+// Few long bags: as many workgroups as the chip holds share all entries evenly, in blocks of kBlock, wherever bags begin and end;
+// a part's fixed cost (the way to its first rows, the meeting of its wavefronts: 8 us in a busy memory) is then paid once and at
+// the same time everywhere, and no CU is left with a part more than another.  (64 bags of 4,096 entries, 1 KB rows: 512 workgroups
+// in order 65 us; bags of up to 8,192: 99 by pieces.)  Bag b's blocks have the numbers [blocks[b], blocks[b + 1]), an empty bag's
+// one block among them; workgroup w takes those from w * all / groups on.
+constexpr int kBlockShift = 7, kBlock = 1 << kBlockShift, kEvenBags = 2048;
+__device__ __forceinline__ uint32_t bag_blocks(const AttnArgs& a, uint32_t bag) {
+    return max(1u, (uint32_t)((bag_span(a, bag).count + kBlock - 1) >> kBlockShift));
+}
+__device__ __forceinline__ uint32_t even_start(uint32_t w, uint32_t all, uint32_t groups) { return (uint32_t)((uint64_t)w * all / groups); }
+__device__ __forceinline__ uint32_t even_owner(uint32_t block, uint32_t all, uint32_t groups) { return (uint32_t)(((uint64_t)(block + 1) * groups - 1) / all); }
+
+template <typename T, int DP, int PACK>
+__global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_even_kernel(FwdArgs f) {
+    extern __shared__ float lds[];
+    __shared__ uint32_t wave_sums[kFwdWaves], start_bag, start_block;
     const AttnArgs& a = f.a;
-    const BagPiece p = find_piece(a, f.shift, blockIdx.x, f.pieces);
-    if (p.number >= p.of || (p.of == 1 && !f.scores)) return;
-    const int hq = a.q_heads, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    float* const best = lds;                      // [hq]
-    float* const total = lds + hq;                // [hq]
-    float* const part = lds + 2 * hq;             // [kFwdBlock]
-    const float* const ml = f.part_ml + (int64_t)p.first_id * hq * 2;
-    for (int h = wave; h < hq; h += kFwdWaves) {
-        float top = -INFINITY;
-        for (uint32_t i = lane; i < p.of; i += 64) top = fmaxf(top, ml[((int64_t)i * hq + h) * 2]);
-        for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-        const float from = top == -INFINITY ? 0.f : top;
-        float l = 0.f;
-        for (uint32_t i = lane; i < p.of; i += 64) l = fmaf(exp_few_ulp(ml[((int64_t)i * hq + h) * 2] - from), ml[((int64_t)i * hq + h) * 2 + 1], l);
-        for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
-        if (lane == 0) {
-            best[h] = from;
-            total[h] = l;
-            if (p.number == 0 && p.of > 1) f.lse[(int64_t)p.bag * hq + h] = l == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(l) * kLn2;
+    const uint32_t bags = (uint32_t)a.bags, per = (bags + kFwdBlock - 1) / kFwdBlock;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    // running counts: a thread up to kEvenBags / kFwdBlock bags side by side
+    uint32_t c[kEvenBags / kFwdBlock], sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEvenBags / kFwdBlock; ++i) {
+        const uint32_t b = threadIdx.x * per + i;
+        c[i] = i < per && b < bags ? bag_blocks(a, b) : 0;
+        sum += c[i];
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t x = __shfl_up(upto, off);
+        if (lane >= off) upto += x;
+    }
+    if (lane == 63) wave_sums[wave] = upto;
+    if (threadIdx.x == 0) start_bag = bags;
+    __syncthreads();
+    uint32_t before = upto - sum, all = 0;
+#pragma unroll
+    for (int x = 0; x < kFwdWaves; ++x) {
+        if (x < wave) before += wave_sums[x];
+        all += wave_sums[x];
+    }
+    uint32_t at = even_start(blockIdx.x, all, f.groups);
+    const uint32_t end = even_start(blockIdx.x + 1, all, f.groups);
+#pragma unroll
+    for (uint32_t i = 0; i < kEvenBags / kFwdBlock; ++i) {
+        const uint32_t b = threadIdx.x * per + i;
+        if (i < per && b < bags) {
+            if (blockIdx.x == 0 && blockIdx.y == 0) f.blocks[b] = before;
+            if (before <= at && at < before + c[i]) {
+                start_bag = b;
+                start_block = at - before;
+            }
+            before += c[i];
+            if (b == bags - 1 && blockIdx.x == 0 && blockIdx.y == 0) f.blocks[bags] = before;
         }
     }
     __syncthreads();
-    if (p.of > 1) {
-        const int width = hq * a.d;               // a multiple of 8
-        const float* const po = f.part_o + (int64_t)p.first_id * width;
-        for (int e0 = p.number * kShare; e0 < width; e0 += p.of * kShare) {
-            const int e = e0 + threadIdx.x % kShare, h = min(e / a.d, hq - 1);
-            float v = 0.f;
-            for (uint32_t i = threadIdx.x / kShare; i < p.of && e < width; i += kFwdBlock / kShare)
-                v = fmaf(exp_few_ulp(ml[((int64_t)i * hq + h) * 2] - best[h]), po[(int64_t)i * width + e], v);
-            part[threadIdx.x] = v;
-            __syncthreads();
-            if (threadIdx.x < kShare && e < width) {
-                for (int i = 1; i < kFwdBlock / kShare; ++i) v += part[i * kShare + threadIdx.x];
-                f.out[(int64_t)p.bag * width + e] = total[h] == 0.f ? 0.f : v / total[h];
-            }
-            __syncthreads();
-        }
-    }
-    if (!f.scores) return;
-    for (int i = threadIdx.x; i < p.count; i += kFwdBlock) {
-        const int64_t k = p.first + i;
-        float add = 0.f;
-        for (int h = 0; h < hq; ++h) {
-            const float e = exp_few_ulp(f.scores[k * hq + h] - best[h]);
-            add += total[h] == 0.f ? 0.f : e / total[h];
-        }
-        f.weight_out[k] = (f.weight_in ? f.weight_in[k] : 0.f) + add;
+    uint32_t bag = start_bag, block = start_block;
+    while (at < end && bag < bags) {
+        const BagSpan s = bag_span(a, bag);
+        const uint32_t mine = max(1u, (uint32_t)((s.count + kBlock - 1) >> kBlockShift)), take = min(mine - block, end - at);
+        const int64_t skip = (int64_t)block << kBlockShift;
+        attend<T, DP, PACK>(f, Segment{bag, 2 * blockIdx.x + (block == 0), s.first + skip, (int)min(s.count - skip, (int64_t)take << kBlockShift), take == mine}, lds);
+        at += take;
+        block = 0;
+        ++bag;
     }
 }
 
-// kv heads that share a workgroup's four wavefronts: whole rows are then read by one workgroup where heads are few.
-int fwd_heads(int kv_heads) { return kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
-// Pieces so small that the launch has two workgroups for every CU, within limits.
-constexpr int kShiftLeast = 7, kShiftMost = 10, kPiecesEnough = 1024;
-int64_t fwd_enough(const bp_attn* at) { return kPiecesEnough / (at->kv_heads / fwd_heads(at->kv_heads)); }
-int fwd_shift(const bp_attn* at, int64_t n) {
-    int shift = kShiftLeast;
-    while (shift < kShiftMost && (n >> shift) > fwd_enough(at)) ++shift;
-    return shift;
+// The parts of a bag of several: a workgroup sums 16 elements of their pooled rows, four a thread and 64 parts side by side, each
+// with the maximum and sum of its head, online as within a part.  Workgroups look through `each` bags for such bags.
+constexpr int kJoinBlock = 256, kShare = 16;
+__global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f, int each) {
+    __shared__ float part[kJoinBlock / 64][4][6];
+    const AttnArgs& a = f.a;
+    const int hq = a.q_heads, width = hq * a.d, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int at = blockIdx.y * kShare + threadIdx.x % 4 * 4, h = min(at / a.d, hq - 1);
+    const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
+    // the parts of a bag, and the number of its i-th
+    const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
+        if (f.groups) {
+            const uint32_t all = f.blocks[a.bags];
+            *first = min(even_owner(f.blocks[bag], all, f.groups), f.groups - 1);
+            return min(even_owner(f.blocks[bag + 1] - 1, all, f.groups), f.groups - 1) - *first + 1;
+        }
+        const BagPiece p = bag_piece(a, f.shift, bag, 0, bag_span(a, bag));
+        *first = p.more;
+        return p.of;
+    };
+    uint32_t first_of = 0;
+    uint64_t several = __ballot(lane < each && mine < a.bags && parts_of((uint32_t)min(mine, a.bags - 1), &first_of) > 1);
+    for (; several; several &= several - 1) {
+        const uint32_t bag = (uint32_t)(bag0 + __ffsll((unsigned long long)several) - 1);
+        uint32_t first;
+        const uint32_t of = parts_of(bag, &first);
+        const auto part_id = [&](uint32_t i) -> int64_t {
+            return f.groups ? 2 * (int64_t)(first + i) + (i == 0) : i == 0 ? bag : (int64_t)first + i - 1;
+        };
+        float top = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        const auto take = [&](float m, float x, const float4& v) {
+            const float next = fmaxf(top, m), from = next == -INFINITY ? 0.f : next;
+            const float ka = exp_few_ulp(top - from), kb = exp_few_ulp(m - from);
+            l = fmaf(l, ka, x * kb);
+            o.x = fmaf(o.x, ka, v.x * kb);
+            o.y = fmaf(o.y, ka, v.y * kb);
+            o.z = fmaf(o.z, ka, v.z * kb);
+            o.w = fmaf(o.w, ka, v.w * kb);
+            top = next;
+        };
+        constexpr int AHEAD = 4;
+        for (uint32_t i0 = threadIdx.x / 4; i0 < of; i0 += kJoinBlock / 4 * AHEAD) {
+            float2 ml[AHEAD];
+            float4 v[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const uint32_t i = i0 + j * (kJoinBlock / 4);
+                const bool have = i < of && at < width;
+                const int64_t id = part_id(i);
+                ml[j] = have ? *reinterpret_cast<const float2*>(f.part_ml + (id * hq + h) * 2) : make_float2(-INFINITY, 0.f);
+                v[j] = have ? *reinterpret_cast<const float4*>(f.part_o + id * width + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) take(ml[j].x, ml[j].y, v[j]);
+        }
+#pragma unroll
+        for (int off = 4; off < 64; off <<= 1)
+            take(__shfl_xor(top, off), __shfl_xor(l, off), make_float4(__shfl_xor(o.x, off), __shfl_xor(o.y, off), __shfl_xor(o.z, off), __shfl_xor(o.w, off)));
+        if (lane < 4) {
+            float* const x = part[wave][lane];
+            x[0] = top, x[1] = l, x[2] = o.x, x[3] = o.y, x[4] = o.z, x[5] = o.w;
+        }
+        __syncthreads();
+        if (threadIdx.x < 4 && at < width) {
+            for (int w = 1; w < kJoinBlock / 64; ++w) {
+                const float* const x = part[w][lane];
+                take(x[0], x[1], make_float4(x[2], x[3], x[4], x[5]));
+            }
+            const bool none = l == 0.f;
+            *reinterpret_cast<float4*>(f.out + (int64_t)bag * width + at) =
+                none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+            if (at % a.d == 0) f.lse[(int64_t)bag * hq + h] = none ? -INFINITY : top + __builtin_amdgcn_logf(l) * kLn2;
+        }
+        __syncthreads();
+    }
 }
+
+// Weights of the entries of the bags that were not whole in one workgroup, from the scores and the bags' final norms: an entry a
+// thread.
+constexpr int kWeightShift = 8;
+__global__ __launch_bounds__(kJoinBlock) void embbag_attn_weight_kernel(FwdArgs f) {
+    const BagPiece p = find_piece(f.a, kWeightShift, blockIdx.x);
+    if (p.number >= p.of || (f.weighed && bag_piece(f.a, f.shift, p.bag, 0, bag_span(f.a, p.bag)).of == 1)) return;
+    add_weights<kJoinBlock>(f, p.bag, p.first, p.count);
+}
+
+// How a call is laid out.
+constexpr int kPieceShift = 9, kLongMean = 1 << kPieceShift;
+struct FwdPlan {
+    int dp, pack, chunks;      // head_dim rounded up; kv heads a workgroup takes, and how many such shares there are
+    bool even;                 // bags of 512 entries and more in the mean, and not so many that each workgroup could not count them
+    uint32_t groups;           // what the chip holds at once
+    FwdPlan(const bp_attn* at, int dtype, int64_t n, int64_t bags) {
+        dp = dtype == BP_F32 ? 16 : 32;
+        while (dp < at->head_dim) dp *= 2;
+        // As many heads as have columns, and registers for two workgroups a CU (of four heads of 64, 32 of 1 KB rows: 120 us with
+        // all four in one workgroup, one a CU, 99 with two).
+        pack = 1;
+        const int group = at->q_heads / at->kv_heads;
+        while (pack < at->kv_heads && 2 * pack * group <= 16 && 2 * pack * dp <= 128 && pack < 8) pack *= 2;
+        chunks = (at->kv_heads + pack - 1) / pack;
+        even = bags <= kEvenBags && n >= kLongMean * std::max<int64_t>(bags, 1);
+        const int flat = pack * dp;
+        groups = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(256 * (flat > 128 ? 1 : flat > 64 ? 2 : 3) / chunks, (n >> kBlockShift) + bags));
+    }
+    // parts that a workspace for n has room for, whatever smaller call it serves
+    static int64_t parts(int64_t n, int64_t bags) { return std::max((n >> kPieceShift) + bags, 2 * std::min<int64_t>(768, (n >> kBlockShift) + std::min<int64_t>(bags, kEvenBags))); }
+};
+
+// From one head's scores to the next: whole lines, and no power of two.
+int64_t score_stride(int64_t n) { return ceil_div(n, 64) * 64 + 192; }
 
 struct FwdScratch {
     float *scores, *part_ml, *part_o;
+    uint32_t* blocks;
     size_t bytes;
     FwdScratch(void* ws, const bp_attn* at, int64_t n, int64_t bags, bool with_weights) {
-        // room for the pieces of any n up to this one: a workspace for the largest call serves the smaller ones
-        const int64_t pieces = bags + std::max(std::min(n >> kShiftLeast, fwd_enough(at)), n >> kShiftMost);
+        const int64_t parts = FwdPlan::parts(n, bags);
         Carver c(ws, 0);
-        scores = c.take<float>(with_weights ? (size_t)n * at->q_heads : 0);
-        part_ml = c.take<float>((size_t)pieces * at->q_heads * 2);
-        part_o = c.take<float>((size_t)pieces * at->q_heads * at->head_dim);
+        scores = c.take<float>(with_weights ? (size_t)score_stride(n) * at->q_heads : 0);
+        part_ml = c.take<float>((size_t)parts * at->q_heads * 2);
+        part_o = c.take<float>((size_t)parts * at->q_heads * at->head_dim);
+        blocks = c.take<uint32_t>((size_t)std::min<int64_t>(bags, kEvenBags) + 1);
         bytes = c.used();
     }
 };
 
-template <typename T, int DP>
-int launch_fwd(const FwdArgs& f, hipStream_t stream) {
-    const int table = f.a.bias ? f.a.rp.rows() * f.heads * (f.a.q_heads / f.a.kv_heads) : 0;
-    BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP>), dim3(f.pieces, (unsigned)(f.a.kv_heads / f.heads)), dim3(kFwdBlock), attn_fwd_lds(DP, table),
-              stream, f);
+template <typename T, int DP, int PACK>
+int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
+    const int table = f.a.bias ? f.a.rp.rows() * std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads) : 0;
+    const size_t shared = AttnLds<kFwdWaves>::bytes(DP * PACK, table);
+    if (l.even)
+        BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+    else
+        BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
     return BP_OK;
 }
-template <typename T>
-int launch_fwd(const FwdArgs& f, hipStream_t stream) {
-    if constexpr (sizeof(T) == 4) {
-        if (f.a.d <= 16) return launch_fwd<T, 16>(f, stream);
+template <typename T, int DP>
+int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
+    switch (l.pack) {
+        case 1: return launch_fwd<T, DP, 1>(f, l, stream);
+        case 2: if constexpr (DP <= 64) return launch_fwd<T, DP, 2>(f, l, stream); break;
+        case 4: if constexpr (DP <= 32) return launch_fwd<T, DP, 4>(f, l, stream); break;
+        case 8: if constexpr (DP <= 16) return launch_fwd<T, DP, 8>(f, l, stream); break;
     }
-    if (f.a.d <= 32) return launch_fwd<T, 32>(f, stream);
-    if (f.a.d <= 64) return launch_fwd<T, 64>(f, stream);
-    if (f.a.d <= 128) return launch_fwd<T, 128>(f, stream);
-    return launch_fwd<T, 256>(f, stream);
+    return fail(BP_ERR_UNSUPPORTED, "no layout for %d heads of %d", l.pack, DP);
+}
+template <typename T>
+int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
+    switch (l.dp) {
+        case 16: if constexpr (sizeof(T) == 4) return launch_fwd<T, 16>(f, l, stream); break;
+        case 32: return launch_fwd<T, 32>(f, l, stream);
+        case 64: return launch_fwd<T, 64>(f, l, stream);
+        case 128: return launch_fwd<T, 128>(f, l, stream);
+    }
+    return launch_fwd<T, 256>(f, l, stream);
 }
 
 }  // namespace
@@ -525,18 +750,29 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     BP_TRY(bp_embbag_attn_fwd_workspace_bytes(cfg, at, n_lookups, bags, weights, &need));
     BP_TRY(attn_check_workspace(workspace, workspace_bytes, need));
     const FwdScratch w(workspace, at, n_lookups, bags, weights);
-    f.shift = fwd_shift(at, n_lookups);
-    f.heads = fwd_heads(at->kv_heads);
+    const FwdPlan l(at, cfg->weight_dtype, n_lookups, bags);
+    f.shift = kPieceShift;
     f.pieces = (uint32_t)piece_count(n_lookups, bags, f.shift);
+    f.groups = l.even ? l.groups : 0;
+    f.blocks = w.blocks;
     f.scores = weights ? w.scores : nullptr;
+    f.spread = spread_of(n_lookups >> f.shift);
+    f.score_stride = score_stride(n_lookups);
+    f.weighed = l.chunks == 1 && !l.even;
     f.part_ml = w.part_ml;
     f.part_o = w.part_o;
     f.out = out;
     f.lse = lse;
     f.weight_in = weight_in;
     f.weight_out = weight_out;
-    BP_TRY(cfg->weight_dtype == BP_F32 ? launch_fwd<float>(f, stream) : launch_fwd<uint16_t>(f, stream));
-    if (weights || n_lookups > (int64_t(1) << f.shift))         // else no bag can have two pieces
-        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_join_kernel, dim3(f.pieces), dim3(kFwdBlock), (size_t)(2 * at->q_heads + kFwdBlock) * 4, stream, f);
+    BP_TRY(cfg->weight_dtype == BP_F32 ? launch_fwd<float>(f, l, stream) : launch_fwd<uint16_t>(f, l, stream));
+    const bool several = l.even ? l.groups > 1 : n_lookups > (int64_t(1) << f.shift);          // else no bag can have two parts
+    if (several) {
+        const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
+        const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);
+        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_join_kernel, dim3((unsigned)ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f, (int)each);
+    }
+    if (weights && (several || !f.weighed))
+        BP_LAUNCH(K_ATTN_WEIGHT, embbag_attn_weight_kernel, dim3((unsigned)piece_count(n_lookups, bags, kWeightShift)), dim3(kJoinBlock), 0, stream, f);
     return BP_OK;
 }
