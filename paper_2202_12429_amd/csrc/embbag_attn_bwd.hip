@@ -1,143 +1,455 @@
 // bp_embbag_attn_bwd: the gradients of bags pooled by attention over their cached rows.
+//
+// One pass over a bag's rows.  With lse and the pooled rows from the forward pass a score's gradient needs no other entry:
+//     p = exp(c - lse),  dz = p * (<grad_out, value> - <grad_out, out>),  ds = dz * (the cap's slope) * scale
+// grad of the key = sum over its heads of ds * q, of the value = sum of p * grad_out, of q = sum over the entries of ds * key,
+// of the bias table = sum of dz by table row.  Bound by memory: a row is read once and its gradient, in fp32, written.
 #include <algorithm>
 #include <cmath>
 
-#include "attn_args.h"
+#include "attn_tile.h"
 
 namespace bp {
 namespace {
 
-// The table row of an entry's distance: -1 when it is not seen, 0 where no bias is asked for.
-__device__ __forceinline__ int entry_row(const AttnArgs& a, int64_t bag, int64_t k, const int32_t* borders) {
-    if ((uint32_t)a.slots[k] >= (uint64_t)a.C) return -1;
-    if (!a.bias) return 0;
-    return relpos_row((int64_t)a.q_pos[bag] - a.lookup_pos[k], borders, a.rp.buckets, a.rp.two_sided);
+// Wavefronts work by themselves: all entries are numbered in units of 32, bag b's from (its offset >> 5) + b on, and shared out
+// evenly, wherever bags begin and end.  A bag that is one wavefront's has its grad_q from there; parts of others meet in a launch
+// of their own.
+constexpr int kUnitShift = 5, kUnit = 1 << kUnitShift;
+constexpr int kBwdWaves = 4, kBwdBlock = kBwdWaves * 64;
+
+struct BwdArgs {
+    AttnArgs a;
+    const float* out;
+    const float* lse;
+    const float* grad_out;
+    float* grad_q;
+    float* grad_rows;
+    uint32_t units, waves;      // (n >> kUnitShift) + bags; wavefronts that share them
+    float* parts;               // [2 * waves][q_heads][d]: grad_q of a bag's part: [2w] of the bag that is under way as wavefront w
+                                // begins, [2w + 1] of the one it begins and does not end
+    float* bias_parts;          // [workgroups][table rows][q_heads]
+};
+
+__device__ __forceinline__ uint32_t first_unit(const AttnArgs& a, uint32_t bag) {
+    int64_t at = a.bag_off[bag];
+    if (at < 0) at = 0;
+    if (at > a.n) at = a.n;
+    return (uint32_t)(at >> kUnitShift) + bag;
+}
+__device__ __forceinline__ uint32_t share_start(uint32_t wave, uint32_t units, uint32_t waves) { return (uint32_t)((uint64_t)wave * units / waves); }
+__device__ __forceinline__ uint32_t share_of(uint32_t unit, uint32_t units, uint32_t waves) {
+    return min((uint32_t)(((uint64_t)(unit + 1) * waves - 1) / units), waves - 1);
 }
 
-constexpr int kAttnBlock = 256;
-constexpr int kMaxQHeads = 1024;
-
-// A workgroup a bag: p and the gradient of the scores to the workspace, then the gradients that they are summed into.
+// LDS: borders, the bias table's columns of the workgroup's heads; of every wavefront a tile's slots and table offsets, its ds and p
+// entry by entry, and four tables of sums, one for each quarter of the wavefront, in which a column is one lane's.
 template <typename T>
-__global__ __launch_bounds__(kAttnBlock) void embbag_attn_bwd_kernel(AttnArgs a, const float* __restrict__ out, const float* __restrict__ lse,
-                                                                     const float* __restrict__ grad_out, float* __restrict__ ps,
-                                                                     float* __restrict__ dzs, int32_t* __restrict__ rows,
-                                                                     float* __restrict__ grad_q, float* __restrict__ grad_rows) {
-    __shared__ int32_t borders[BP_RELPOS_MAX_BUCKETS];
-    __shared__ float against[kMaxQHeads];
-    if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = a.rp.borders[threadIdx.x];
-    const int64_t bag = blockIdx.x;
-    const BagSpan s = bag_span(a, bag);
-    const T* const w = (const T*)a.cache_w;
-    const int hq = a.q_heads, group = hq / a.kv_heads;
-    for (int h = threadIdx.x; h < hq; h += kAttnBlock) {
-        float sum = 0.f;
-        for (int i = 0; i < a.d; ++i) sum = fmaf(grad_out[(bag * hq + h) * a.d + i], out[(bag * hq + h) * a.d + i], sum);
-        against[h] = sum;
-    }
-    __syncthreads();
-    for (int64_t e = threadIdx.x; e < s.count * hq; e += kAttnBlock) {
-        const int64_t k = s.first + e / hq;
-        const int h = (int)(e % hq);
-        const int row = entry_row(a, bag, k, borders);
-        if (h == 0) rows[k] = row;
-        float p = 0.f, dz = 0.f, ds = 0.f;
-        if (row >= 0) {
-            const T* const key = w + a.slots[k] * a.wst + (h / group) * a.d;
-            const T* const val = key + a.value_at;
-            const float* const q = a.q + (bag * hq + h) * a.d;
-            const float* const g = grad_out + (bag * hq + h) * a.d;
-            float dot = 0.f, dp = 0.f;
-            for (int i = 0; i < a.d; ++i) {
-                dot = fmaf(q[i], row_value(key, i), dot);
-                dp = fmaf(g[i], row_value(val, i), dp);
-            }
-            float c = a.scale * dot, bend = 1.f;
-            if (a.cap > 0) {
-                const float t = tanhf(c / a.cap);
-                c = a.cap * t;
-                bend = 1.f - t * t;
-            }
-            if (a.bias) c += a.bias[row * hq + h];
-            p = c == -INFINITY ? 0.f : expf(c - lse[bag * hq + h]);
-            dz = p * (dp - against[h]);
-            ds = dz * bend * a.scale;
-        }
-        ps[k * hq + h] = p;
-        dzs[(k * hq + h) * 2] = dz;
-        dzs[(k * hq + h) * 2 + 1] = ds;
-    }
-    __syncthreads();
-    for (int t = threadIdx.x; t < hq * a.d; t += kAttnBlock) {
-        const int h = t / a.d, i = t % a.d;
-        float sum = 0.f;
-        for (int64_t k = s.first; k < s.first + s.count; ++k)
-            if (rows[k] >= 0) sum = fmaf(dzs[(k * hq + h) * 2 + 1], row_value(w + a.slots[k] * a.wst + (h / group) * a.d, i), sum);
-        grad_q[bag * hq * a.d + t] = sum;
-    }
-    const int span = a.kv_heads * a.d;
-    for (int64_t t = threadIdx.x; t < s.count * a.dim; t += kAttnBlock) {
-        const int64_t k = s.first + t / a.dim;
-        const int i = (int)(t % a.dim);
-        float sum = 0.f;
-        if (rows[k] >= 0) {
-            if (i < span)
-                for (int h = i / a.d * group; h < (i / a.d + 1) * group; ++h)
-                    sum = fmaf(dzs[(k * hq + h) * 2 + 1], a.q[(bag * hq + h) * a.d + i % a.d], sum);
-            const int v = i - a.value_at;
-            if (v >= 0 && v < span)
-                for (int h = v / a.d * group; h < (v / a.d + 1) * group; ++h)
-                    sum = fmaf(ps[k * hq + h], grad_out[(bag * hq + h) * a.d + v % a.d], sum);
-        }
-        grad_rows[k * a.dim + i] = sum;
-    }
-}
+struct BwdLds {
+    static constexpr int ROWS = sizeof(T) == 2 ? 32 : 16, WIDE = 17;
+    static constexpr int TILE = 64, TURN = TILE + 64, EACH = 64 + 2 * ROWS * WIDE;      // of a wavefront behind the borders
+    static size_t floats(int table_rows, int cols) { return 64 + (size_t)kBwdWaves * EACH + (size_t)table_rows * cols + (size_t)kBwdWaves * 4 * table_rows * 16; }
+};
 
-__global__ __launch_bounds__(256) void attn_clear_rows_kernel(int32_t* __restrict__ rows, int64_t n) {
-    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (k < n) rows[k] = -1;
-}
+template <typename T, int DP, int PACK>
+__global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn_bwd_kernel(BwdArgs f) {
+    typedef AttnTile<T, DP, PACK> X;
+    typedef BwdLds<T> L;
+    typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
+    constexpr int STEPS = PACK == 1 ? 4 : PACK == 2 ? 2 : 1;             // of four columns, in a head's group
+    constexpr int BLOCKS = DP / 16;                                      // of 16 elements of a head
+    extern __shared__ float lds[];
+    const AttnArgs& a = f.a;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = min(PACK, a.kv_heads - kv0);
+    const int first_head = kv0 * group, cols = heads * group, flat = heads * a.d, span = a.kv_heads * a.d;
+    const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;
+    const int table_rows = a.bias ? a.rp.rows() : 0;
 
-// Table gradient of one head over one share of the entries: a column a lane, so that no two lanes meet.
-constexpr int kBiasShares = 256;
-__global__ __launch_bounds__(64) void attn_bias_grad_kernel(const float* __restrict__ dzs, const int32_t* __restrict__ rows, int64_t n, int hq,
-                                                            int table_rows, double* __restrict__ partial) {
-    __shared__ float sums[2 * BP_RELPOS_MAX_BUCKETS][64];
-    const int lane = threadIdx.x, h = blockIdx.y;
-    for (int r = 0; r < table_rows; ++r) sums[r][lane] = 0.f;
-    const int64_t share = (n + kBiasShares - 1) / kBiasShares;
-    for (int64_t k = blockIdx.x * share + lane; k < min(n, (blockIdx.x + 1) * share); k += 64) {
-        const int r = rows[k];
-        if (r >= 0) sums[r][lane] += dzs[(k * hq + h) * 2];
+    int32_t* const borders = (int32_t*)lds;
+    int32_t* const tile = (int32_t*)lds + 64 + wave * L::EACH;           // slots, then table offsets
+    float* const turn_ds = lds + 64 + wave * L::EACH + 64;               // [entry][column]
+    float* const turn_p = turn_ds + L::ROWS * L::WIDE;
+    float* const table = lds + 64 + kBwdWaves * L::EACH;
+    float* const sums = table + table_rows * cols + wave * 4 * table_rows * 16 + g * table_rows * 16 + col;      // this lane's column
+    if (a.bias) {
+        if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = a.rp.borders[threadIdx.x];
+        for (int e = threadIdx.x; e < table_rows * cols; e += kBwdBlock) table[e] = a.bias[(e / cols) * a.q_heads + first_head + e % cols];
+        for (int r = 0; r < table_rows; ++r) sums[r * 16] = 0.f;
+        __syncthreads();
     }
+
+    const uint32_t share = blockIdx.x * kBwdWaves + wave;
+    uint32_t at = share < f.waves ? share_start(share, f.units, f.waves) : f.units;
+    const uint32_t end = share < f.waves ? share_start(share + 1, f.units, f.waves) : f.units;
+    uint32_t bag = 0;
+    if (at < end) {
+        uint32_t hi = (uint32_t)a.bags;
+        while (hi - bag > 1) {                                           // the last bag that begins no later, 64 bags a step
+            const uint32_t step = (hi - bag + 63) / 64, i = bag + (lane + 1) * step;
+            bag += __popcll(__ballot(i < hi && first_unit(a, i) <= at)) * step;
+            hi = min(hi, bag + step);
+        }
+    }
+    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * a.d;
+    const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
+    int sum_row = -1;                                                    // the lane's running sum for the bias table, and its row
+    float sum_dz = 0.f;
+
+    for (; at < end && bag < (uint32_t)a.bags; ++bag) {
+        // the bag's units from `at` on that are this wavefront's
+        const BagSpan s = bag_span(a, bag);
+        const uint32_t from = first_unit(a, bag), mine = max(1u, (uint32_t)((s.count + kUnit - 1) >> kUnitShift));
+        const uint32_t begin = at - min(at, from), stop = min(mine, end - min(end, from));
+        const bool starts = begin == 0, whole = starts && stop == mine;
+        at = bag + 1 < (uint32_t)a.bags ? max(at, first_unit(a, bag + 1)) : end;
+        if (begin >= stop) continue;                                     // numbers without a unit
+        const int64_t first = s.first + ((int64_t)begin << kUnitShift);
+        const int count = (int)min(s.count - ((int64_t)begin << kUnitShift), (int64_t)(stop - begin) << kUnitShift);
+
+        // q and grad_out: for the products with rows, and (a column a quarter) for those with ds and p
+        const float* const q = a.q + ((int64_t)bag * a.q_heads + head) * a.d;
+        const float* const go = f.grad_out + ((int64_t)bag * a.q_heads + head) * a.d;
+        const float* const po = f.out + ((int64_t)bag * a.q_heads + head) * a.d;
+        std::conditional_t<X::BF16, Split3, f32x4> qf[X::KM], gf[X::KM];
+        float against = 0.f;                                             // <grad_out, out> of the column
+#pragma unroll
+        for (int m = 0; m < X::KM; ++m) {
+            const int x = m * X::KC + g * (X::KC / 4);
+            const bool have = col < cols && x < a.d;
+            constexpr int VECS = X::BF16 ? 2 : 1;
+            float v[4 * VECS], u[4 * VECS];
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) {
+                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4 tq = have ? *reinterpret_cast<const float4*>(q + x + 4 * i) : zero;
+                const float4 tg = have ? *reinterpret_cast<const float4*>(go + x + 4 * i) : zero;
+                const float4 to = have ? *reinterpret_cast<const float4*>(po + x + 4 * i) : zero;
+                v[4 * i] = tq.x, v[4 * i + 1] = tq.y, v[4 * i + 2] = tq.z, v[4 * i + 3] = tq.w;
+                u[4 * i] = tg.x, u[4 * i + 1] = tg.y, u[4 * i + 2] = tg.z, u[4 * i + 3] = tg.w;
+                against = fmaf(tg.x, to.x, fmaf(tg.y, to.y, fmaf(tg.z, to.z, fmaf(tg.w, to.w, against))));
+            }
+            if constexpr (X::BF16) {
+                qf[m].set(v);
+                gf[m].set(u);
+            } else {
+                qf[m] = f32x4{v[0], v[1], v[2], v[3]};
+                gf[m] = f32x4{u[0], u[1], u[2], u[3]};
+            }
+        }
+        against += __shfl_xor(against, 16);
+        against += __shfl_xor(against, 32);
+        const float lse = f.lse[(int64_t)bag * a.q_heads + head];
+        float qt[PACK][BLOCKS][STEPS], gt[PACK][BLOCKS][STEPS];          // element 16 * block + col of head k's column 4 * step + g
+#pragma unroll
+        for (int k = 0; k < PACK; ++k)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const int c = 4 * t + g, x = 16 * b + col;
+                    const bool have = k < heads && c < group && x < a.d;
+                    const int64_t place = ((int64_t)bag * a.q_heads + first_head + k * group + c) * a.d + x;
+                    qt[k][b][t] = have ? a.q[place] : 0.f;
+                    gt[k][b][t] = have ? f.grad_out[place] : 0.f;
+                }
+        const int64_t q_pos = a.bias ? a.q_pos[bag] : 0;
+
+        f32x4 dq[X::MB][X::VW];
+#pragma unroll
+        for (int m = 0; m < X::MB; ++m)
+#pragma unroll
+            for (int j = 0; j < X::VW; ++j) dq[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        for (int e0 = 0; e0 < count; e0 += X::ROWS) {
+            int row_of = -1, slot = -1;
+            if (lane < X::ROWS && e0 + lane < count) slot = a.slots[first + e0 + lane];
+            if ((uint32_t)slot < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - a.lookup_pos[first + e0 + lane], borders, a.rp.buckets, a.rp.two_sided) : 0;
+            const uint64_t seen = __ballot(row_of >= 0);
+            const bool all_seen = seen == (X::ROWS == 32 ? 0xffffffffull : 0xffffull);
+            __builtin_amdgcn_wave_barrier();
+            if (lane < X::ROWS) {
+                tile[lane] = row_of >= 0 ? slot : 0;                     // what is not seen reads row 0, and leaves it out
+                tile[32 + lane] = row_of;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            // scores and <grad_out, value>, each entry's against every column
+            float c[X::PER], dp[X::PER];
+#pragma unroll
+            for (int u = 0; u < X::NU; ++u) {
+                const T* const row = w + (int64_t)tile[X::PER * (col / 4) + 4 * u + col % 4] * a.wst;
+                uint4 kr[PACK][X::KM], vr[PACK][X::KM];
+#pragma unroll
+                for (int k = 0; k < PACK; ++k)
+#pragma unroll
+                    for (int m = 0; m < X::KM; ++m) {
+                        const int x = m * X::KC + g * (X::KC / 4);
+                        const bool have = x < a.d && k < heads;
+                        kr[k][m] = have ? *reinterpret_cast<const uint4*>(row + k * a.d + x) : make_uint4(0, 0, 0, 0);
+                        vr[k][m] = have ? *reinterpret_cast<const uint4*>(row + a.value_at + k * a.d + x) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                for (int k = 0; k < PACK; ++k) {
+                    f32x4 sc = {0.f, 0.f, 0.f, 0.f}, sp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int m = 0; m < X::KM; ++m) {
+                        if constexpr (X::BF16) {
+#pragma unroll
+                            for (int part = 2; part >= 0; --part) {
+                                sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[k][m]), qf[m].part[part], sc, 0, 0, 0);
+                                sp = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[k][m]), gf[m].part[part], sp, 0, 0, 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kr[k][m], i)), qf[m][i], sc, 0, 0, 0);
+                                sp = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vr[k][m], i)), gf[m][i], sp, 0, 0, 0);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        c[4 * u + i] = k == 0 || own == k ? sc[i] : c[4 * u + i];
+                        dp[4 * u + i] = k == 0 || own == k ? sp[i] : dp[4 * u + i];
+                    }
+                }
+            }
+            // the keys again, in whole rows (from the caches)
+            VRaw kv[X::PER][X::MB];
+#pragma unroll
+            for (int e = 0; e < X::PER; ++e) {
+                const T* const row = w + (int64_t)tile[X::PER * g + e] * a.wst;
+#pragma unroll
+                for (int m = 0; m < X::MB; ++m) {
+                    const int x = m * 16 * X::VW + col * X::VW;
+                    kv[e][m] = *reinterpret_cast<const VRaw*>(row + (x < flat ? x : 0));
+                }
+            }
+            float ds[X::PER];
+#pragma unroll
+            for (int e = 0; e < X::PER; ++e) {
+                const int r = tile[32 + X::PER * g + e];
+                float z = c[e] * a.scale, bend = a.scale;
+                if (a.cap > 0) {
+                    const float t = tanh_few_ulp(c[e] * by_cap);
+                    z = a.cap * t;
+                    bend *= fmaf(-t, t, 1.f);
+                }
+                if (a.bias) z += table[max(r, 0) * cols + min(col, cols - 1)];
+                const bool in = r >= 0 && z != -INFINITY;                // (a score of -infinity weighs nothing, also in a bag of them alone)
+                // A weight that rounds to 1 has all others below a rounding, and its score no gradient but the two products' difference in
+                // rounding, which a step of Adagrad would blow up (bags of one entry).
+                const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in && p != 1.f ? p * (dp[e] - against) : 0.f;
+                ds[e] = dz * bend;
+                turn_ds[(X::PER * g + e) * L::WIDE + col] = ds[e];
+                turn_p[(X::PER * g + e) * L::WIDE + col] = p;
+                if (a.bias && r >= 0 && col < cols) {
+                    if (r != sum_row) {
+                        if (sum_row >= 0) sums[sum_row * 16] += sum_dz;
+                        sum_row = r;
+                        sum_dz = 0.f;
+                    }
+                    sum_dz += dz;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            // gradients of the rows: elements down (four side by side a lane), entries across
+#pragma unroll
+            for (int u = 0; u < X::NU; ++u) {
+                const int entry = 16 * u + col;
+                const bool mine_seen = seen >> entry & 1;
+                float* const to = f.grad_rows + (first + e0 + entry) * a.dim + kv0 * a.d;
+#pragma unroll
+                for (int k = 0; k < PACK; ++k) {
+                    float x_ds[STEPS], x_p[STEPS];
+#pragma unroll
+                    for (int t = 0; t < STEPS; ++t) {
+                        const bool have = k < heads && 4 * t + g < group;
+                        x_ds[t] = have ? turn_ds[entry * L::WIDE + k * group + 4 * t + g] : 0.f;
+                        x_p[t] = have ? turn_p[entry * L::WIDE + k * group + 4 * t + g] : 0.f;
+                    }
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) {
+                        f32x4 gk = {0.f, 0.f, 0.f, 0.f}, gv = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int t = 0; t < STEPS; ++t) {
+                            if (4 * t >= group) continue;
+                            gk = __builtin_amdgcn_mfma_f32_16x16x4f32(qt[k][b][t], x_ds[t], gk, 0, 0, 0);
+                            gv = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[k][b][t], x_p[t], gv, 0, 0, 0);
+                        }
+                        const int x = 16 * b + 4 * g;
+                        if (k < heads && x < a.d && e0 + entry < count) {
+                            if (!mine_seen) gk = gv = f32x4{0.f, 0.f, 0.f, 0.f};
+                            if (a.value_at == 0) {
+                                *reinterpret_cast<f32x4*>(to + k * a.d + x) = gk + gv;
+                            } else {
+                                *reinterpret_cast<f32x4*>(to + k * a.d + x) = gk;
+                                *reinterpret_cast<f32x4*>(to + a.value_at + k * a.d + x) = gv;
+                            }
+                        }
+                    }
+                }
+            }
+            // of q: as the forward pass pools values
+            if (!all_seen) {
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e)
+#pragma unroll
+                    for (int m = 0; m < X::MB; ++m) kv[e][m] = masked(kv[e][m], seen >> (X::PER * g + e) & 1 ? ~0u : 0u);
+            }
+            if constexpr (X::BF16) {
+                Split3 df;
+                df.set(ds);
+#pragma unroll
+                for (int m = 0; m < X::MB; ++m)
+#pragma unroll
+                    for (int j = 0; j < X::VW; ++j) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[i] = __builtin_amdgcn_perm(word(kv[2 * i + 1][m], j / 2), word(kv[2 * i][m], j / 2), j % 2 ? 0x07060302u : 0x05040100u);
+                        const bf16x8 kf = __builtin_bit_cast(bf16x8, make_uint4(v[0], v[1], v[2], v[3]));
+#pragma unroll
+                        for (int part = 2; part >= 0; --part) dq[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, df.part[part], dq[m][j], 0, 0, 0);
+                    }
+            } else {
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e)
+#pragma unroll
+                    for (int m = 0; m < X::MB; ++m)
+#pragma unroll
+                        for (int j = 0; j < X::VW; ++j)
+                            dq[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kv[e][m], j)), ds[e], dq[m][j], 0, 0, 0);
+            }
+        }
+        // elements of the rows that are neither key nor value
+        const int behind = a.value_at + span, gap = a.value_at == 0 ? 0 : a.value_at - span;
+        if (blockIdx.y == 0 && gap + a.dim - behind > 0)
+            for (int64_t e = lane; e < (int64_t)count * (gap + a.dim - behind); e += 64) {
+                const int x = (int)(e % (gap + a.dim - behind));
+                f.grad_rows[(first + e / (gap + a.dim - behind)) * a.dim + (x < gap ? span + x : behind + x - gap)] = 0.f;
+            }
+        float* const to = (whole ? f.grad_q + ((int64_t)bag * a.q_heads + head) * a.d
+                                 : f.parts + ((2 * (int64_t)share + starts) * a.q_heads + head) * a.d) - own * a.d;
+#pragma unroll
+        for (int m = 0; m < X::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = (m * 16 + 4 * g + i) * X::VW;
+                float v[X::VW];
+#pragma unroll
+                for (int j = 0; j < X::VW; ++j) v[j] = dq[m][j][i];
+                if (col < cols && x >= own * a.d && x < (own + 1) * a.d) __builtin_memcpy(__builtin_assume_aligned(to + x, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+            }
+    }
+    if (!a.bias) return;
+    if (sum_row >= 0 && col < cols) sums[sum_row * 16] += sum_dz;
     __syncthreads();
-    for (int r = lane; r < table_rows; r += 64) {
+    const float* const all = table + table_rows * cols;
+    for (int e = threadIdx.x; e < table_rows * cols; e += kBwdBlock) {
         double sum = 0;
-        for (int j = 0; j < 64; ++j) sum += sums[r][j];
-        partial[((int64_t)blockIdx.x * table_rows + r) * hq + h] = sum;
+        for (int x = 0; x < kBwdWaves * 4; ++x) sum += all[(x * table_rows + e / cols) * 16 + e % cols];
+        f.bias_parts[((int64_t)blockIdx.x * table_rows + e / cols) * a.q_heads + first_head + e % cols] = (float)sum;
     }
 }
 
-__global__ __launch_bounds__(256) void attn_bias_join_kernel(const double* __restrict__ partial, int count, float* __restrict__ grad_bias) {
-    const int e = blockIdx.x * 256 + threadIdx.x;
-    if (e >= count) return;
-    double sum = 0;
-    for (int s = 0; s < kBiasShares; ++s) sum += partial[(int64_t)s * count + e];
-    grad_bias[e] = (float)sum;
+// grad_q of the bags that several wavefronts had a part of: a workgroup 16 elements, four a thread and 64 parts side by side; it
+// looks through `each` bags for such bags.
+constexpr int kJoinBlock = 256, kShare = 16;
+__global__ __launch_bounds__(kJoinBlock) void embbag_attn_bwd_join_kernel(BwdArgs f, int each) {
+    __shared__ float4 part[kJoinBlock / 64][4];
+    const AttnArgs& a = f.a;
+    const int width = a.q_heads * a.d, lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = blockIdx.y * kShare + threadIdx.x % 4 * 4;
+    const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
+    const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
+        const uint32_t from = first_unit(a, bag), units = max(1u, (uint32_t)((bag_span(a, bag).count + kUnit - 1) >> kUnitShift));
+        *first = share_of(from, f.units, f.waves);
+        return share_of(min(from + units, f.units) - 1, f.units, f.waves) - *first + 1;
+    };
+    uint32_t first = 0;
+    uint64_t several = __ballot(lane < each && mine < a.bags && parts_of((uint32_t)min(mine, a.bags - 1), &first) > 1);
+    for (; several; several &= several - 1) {
+        const uint32_t bag = (uint32_t)(bag0 + __ffsll((unsigned long long)several) - 1), of = parts_of(bag, &first);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t i = threadIdx.x / 4; i < of && at < width; i += kJoinBlock / 4) {
+            const float4 x = *reinterpret_cast<const float4*>(f.parts + (2 * (int64_t)(first + i) + (i == 0)) * width + at);
+            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+        }
+#pragma unroll
+        for (int off = 4; off < 64; off <<= 1) {
+            v.x += __shfl_xor(v.x, off);
+            v.y += __shfl_xor(v.y, off);
+            v.z += __shfl_xor(v.z, off);
+            v.w += __shfl_xor(v.w, off);
+        }
+        if (lane < 4) part[wave][lane] = v;
+        __syncthreads();
+        if (threadIdx.x < 4 && at < width) {
+            for (int x = 1; x < kJoinBlock / 64; ++x) {
+                const float4 y = part[x][lane];
+                v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+            }
+            *reinterpret_cast<float4*>(f.grad_q + (int64_t)bag * width + at) = v;
+        }
+        __syncthreads();
+    }
 }
+
+// grad_bias from the workgroups' parts: 16 elements of the table a workgroup, 16 parts of them side by side
+__global__ __launch_bounds__(256) void embbag_attn_bias_join_kernel(const float* __restrict__ parts, int count, int groups, float* __restrict__ grad_bias) {
+    __shared__ double part[16][16];
+    const int c = threadIdx.x % 16, e = blockIdx.x * 16 + c, share = threadIdx.x / 16;
+    double sum = 0;
+    if (e < count)
+        for (int x = share; x < groups; x += 16) sum += parts[(int64_t)x * count + e];
+    part[share][c] = sum;
+    __syncthreads();
+    if (share == 0 && e < count) {
+        for (int x = 1; x < 16; ++x) sum += part[x][c];
+        grad_bias[e] = (float)sum;
+    }
+}
+
+struct BwdPlan {
+    int dp, pack, chunks;
+    uint32_t units, waves, groups;
+    BwdPlan(const bp_attn* at, int dtype, int64_t n, int64_t bags) {
+        dp = attn_dp(at, dtype);
+        pack = attn_pack(at, dp);
+        chunks = (at->kv_heads + pack - 1) / pack;
+        units = (uint32_t)((n >> kUnitShift) + bags);
+        waves = (uint32_t)std::min<int64_t>(units, most_waves(dp, pack, chunks));
+        groups = (waves + kBwdWaves - 1) / kBwdWaves;
+    }
+    // what the chip holds at once
+    static int64_t most_waves(int dp, int pack, int chunks) { return std::max<int64_t>(1, 1024 * (dp * pack > 64 ? 1 : 2) / chunks); }
+};
 
 struct BwdScratch {
-    float *ps, *dzs;
-    int32_t* rows;
-    double* partial;
+    float *parts, *bias_parts;
     size_t bytes;
-    BwdScratch(void* ws, int64_t n, int hq, int table_rows) {
+    BwdScratch(void* ws, const BwdPlan& l, const bp_attn* at, int table_rows) {
         Carver c(ws, 0);
-        ps = c.take<float>((size_t)n * hq);
-        dzs = c.take<float>((size_t)n * hq * 2);
-        rows = c.take<int32_t>((size_t)n);
-        partial = c.take<double>((size_t)kBiasShares * table_rows * hq);
+        parts = c.take<float>((size_t)2 * l.waves * at->q_heads * at->head_dim);
+        bias_parts = c.take<float>((size_t)l.groups * table_rows * at->q_heads);
         bytes = c.used();
+    }
+};
+
+struct BwdLaunch {
+    const BwdArgs& f;
+    const BwdPlan& l;
+    hipStream_t stream;
+    template <typename T, int DP, int PACK>
+    int run() {
+        const int cols = std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads);
+        const size_t shared = BwdLds<T>::floats(f.a.bias ? f.a.rp.rows() : 0, cols) * 4;
+        BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_kernel<T, DP, PACK>), dim3(l.groups, (unsigned)l.chunks), dim3(kBwdBlock), shared, stream, f);
+        return BP_OK;
     }
 };
 
@@ -152,7 +464,7 @@ BP_EXPORT int bp_embbag_attn_bwd_workspace_bytes(const bp_config* cfg, const bp_
     BP_TRY(attn_check_shape(cfg, at));
     BP_TRY(attn_check_sizes(n_lookups, bags, bytes));
     if (rp) BP_TRY(check_relpos(rp, &r));
-    *bytes = BwdScratch(nullptr, n_lookups, at->q_heads, rp ? r.rows() : 0).bytes;
+    *bytes = BwdScratch(nullptr, BwdPlan(at, cfg->weight_dtype, n_lookups, bags), at, rp ? r.rows() : 0).bytes;
     return BP_OK;
 }
 
@@ -161,33 +473,40 @@ BP_EXPORT int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const 
                                  const int32_t* q_pos, const int32_t* lookup_pos, const float* bias_table, const float* out, const float* lse,
                                  const float* grad_out, float* grad_q, float* grad_rows, float* grad_bias, void* workspace,
                                  size_t workspace_bytes, void* stream_) {
-    AttnArgs a;
+    BwdArgs f{};
     size_t need = 0;
     hipStream_t stream = (hipStream_t)stream_;
-    BP_TRY(attn_check(cfg, at, rp, cache_w, lookup_slots, bag_offsets, bag_lengths, n_lookups, bags, q, q_pos, lookup_pos, bias_table, &a));
+    BP_TRY(attn_check(cfg, at, rp, cache_w, lookup_slots, bag_offsets, bag_lengths, n_lookups, bags, q, q_pos, lookup_pos, bias_table, &f.a));
     if ((rp != nullptr) != (grad_bias != nullptr)) return fail(BP_ERR_INVALID_ARG, "grad_bias goes with rp");
     if (bags && (!out || !lse || !grad_out || !grad_q || (n_lookups && !grad_rows))) return fail(BP_ERR_INVALID_ARG, "NULL pointer");
     if ((((uintptr_t)out | (uintptr_t)grad_out | (uintptr_t)grad_q | (uintptr_t)grad_rows) & 15) || (((uintptr_t)lse | (uintptr_t)grad_bias) & 3))
         return fail(BP_ERR_INVALID_ARG, "out, grad_out, grad_q and grad_rows must be 16-byte aligned, lse and grad_bias aligned to their elements");
     BP_TRY(bp_embbag_attn_bwd_workspace_bytes(cfg, at, rp, n_lookups, bags, &need));
     BP_TRY(attn_check_workspace(workspace, workspace_bytes, need));
-    const int table_rows = rp ? a.rp.rows() : 0;
-    const BwdScratch w(workspace, n_lookups, a.q_heads, table_rows);
-    if (n_lookups)
-        BP_LAUNCH(K_FILL, attn_clear_rows_kernel, dim3((unsigned)ceil_div(n_lookups, 256)), dim3(256), 0, stream, w.rows, n_lookups);
+    const BwdPlan l(at, cfg->weight_dtype, n_lookups, bags);
+    const int table_rows = rp ? f.a.rp.rows() : 0, count = table_rows * at->q_heads;
+    const BwdScratch w(workspace, l, at, table_rows);
+    f.out = out;
+    f.lse = lse;
+    f.grad_out = grad_out;
+    f.grad_q = grad_q;
+    f.grad_rows = grad_rows;
+    f.units = l.units;
+    f.waves = l.waves;
+    f.parts = w.parts;
+    f.bias_parts = w.bias_parts;
     if (bags) {
-        const dim3 grid((unsigned)bags), block(kAttnBlock);
-        if (cfg->weight_dtype == BP_F32)
-            BP_LAUNCH(K_ATTN_BWD, embbag_attn_bwd_kernel<float>, grid, block, 0, stream, a, out, lse, grad_out, w.ps, w.dzs, w.rows, grad_q, grad_rows);
-        else
-            BP_LAUNCH(K_ATTN_BWD, embbag_attn_bwd_kernel<uint16_t>, grid, block, 0, stream, a, out, lse, grad_out, w.ps, w.dzs, w.rows, grad_q,
-                      grad_rows);
+        BwdLaunch launch{f, l, stream};
+        BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(l.dp, l.pack, launch) : dispatch_attn<uint16_t>(l.dp, l.pack, launch));
+        if (l.waves > 1) {
+            const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
+            const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);
+            BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bwd_join_kernel, dim3((unsigned)ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f,
+                      (int)each);
+        }
     }
-    if (rp) {
-        const int count = table_rows * a.q_heads;
-        BP_LAUNCH(K_ATTN_JOIN, attn_bias_grad_kernel, dim3(kBiasShares, (unsigned)a.q_heads), dim3(64), 0, stream, w.dzs, w.rows, n_lookups,
-                  a.q_heads, table_rows, w.partial);
-        BP_LAUNCH(K_ATTN_JOIN, attn_bias_join_kernel, dim3((unsigned)ceil_div(count, 256)), dim3(256), 0, stream, w.partial, count, grad_bias);
-    }
+    if (rp)
+        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bias_join_kernel, dim3((unsigned)ceil_div(count, 16)), dim3(256), 0, stream, w.bias_parts, count,
+                  bags ? (int)l.groups : 0, grad_bias);
     return BP_OK;
 }

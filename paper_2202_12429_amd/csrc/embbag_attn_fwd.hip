@@ -4,9 +4,8 @@
 // entries, a workgroup each; the pieces of a bag of several are joined by a second launch, which also turns scores into weights.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
-#include "attn_args.h"
+#include "attn_tile.h"
 
 namespace bp {
 
@@ -85,9 +84,6 @@ int attn_check_sizes(int64_t n, int64_t bags, size_t* bytes) {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 struct FwdArgs {
     AttnArgs a;
     int32_t shift;              // log2 of a piece's entries
@@ -103,53 +99,6 @@ struct FwdArgs {
     float* lse;
     const float* weight_in;
     float* weight_out;
-};
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-// Three bf16 parts of an fp32 value whose sum it is exactly: the leading eight bits of what the parts before leave.
-__device__ __forceinline__ float leading(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
-    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-}
-struct Split3 {
-    bf16x8 part[3];             // 8 values: leading, middle and last bits
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-        uint32_t w[3][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float a = x[2 * i], b = x[2 * i + 1];
-#pragma unroll
-            for (int s = 0; s < 3; ++s) {
-                w[s][i] = upper_halves(a, b);
-                a -= leading(a);
-                b -= leading(b);
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < 3; ++s) part[s] = __builtin_bit_cast(bf16x8, make_uint4(w[s][0], w[s][1], w[s][2], w[s][3]));
-    }
-};
-
-// How a wavefront takes a tile of rows with the matrix instructions: the rows' entries down, query heads across, of which there
-// are up to 16 columns: the groups of PACK kv heads, so that what is done with a score is done for all of them at once.
-// Scores: S[entry][column] = K Q^T for every kv head, of which a column takes its own head's; a lane loads 16 bytes of a row and
-// its neighbours 16 lanes away the next 16.  (A product of all heads' keys with a query padded by zeros would do without the
-// choice, but a NaN of one head would be another's too.)  Pooling: O^T[element][column] = V^T P^T over the heads' values side by
-// side, of which a column's own are taken at the end; an entry whose scores a lane holds is one whose p that lane is asked for,
-// so p never leaves its lane, and V comes in whole rows: a lane loads VW elements, which serve VW products of 16 elements each.
-// bf16 rows go through the bf16 instruction: q and p are cut into three bf16 parts, whose products are exact in fp32, so that
-// what is computed is fp32.  DP: head_dim rounded up.
-template <typename T, int DP, int PACK>
-struct AttnTile {
-    static constexpr bool BF16 = sizeof(T) == 2;
-    static constexpr int ROWS = BF16 ? 32 : 16;        // entries of a tile
-    static constexpr int NU = ROWS / 16;               // S tiles
-    static constexpr int PER = ROWS / 4;               // entries a lane holds scores of
-    static constexpr int KC = BF16 ? 32 : 16, KM = (DP + KC - 1) / KC;
-    static constexpr int FLAT = PACK * DP;             // elements of the heads' values
-    static constexpr int VW = FLAT / 16 < (BF16 ? 8 : 4) ? FLAT / 16 : BF16 ? 8 : 4, MB = FLAT / (16 * VW);
-    static constexpr int OREGS = MB * VW * 4;
 };
 
 // weight_out of a piece's entries, a thread each, from the scores and the bag's norms.  A bag without one (nothing seen) has scores
@@ -168,17 +117,6 @@ __device__ __forceinline__ void add_weights(const FwdArgs& f, uint32_t bag, int6
         f.weight_out[k] = (f.weight_in ? f.weight_in[k] : 0.f) + add;
     }
 }
-
-template <int BYTES>
-struct Bytes {
-    typedef std::conditional_t<BYTES == 16, uint4, std::conditional_t<BYTES == 8, uint2, uint32_t>> type;
-};
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ uint32_t word(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
-__device__ __forceinline__ uint32_t word(uint32_t v, int) { return v; }
-__device__ __forceinline__ uint4 masked(const uint4& v, uint32_t m) { return make_uint4(v.x & m, v.y & m, v.z & m, v.w & m); }
-__device__ __forceinline__ uint2 masked(const uint2& v, uint32_t m) { return make_uint2(v.x & m, v.y & m); }
-__device__ __forceinline__ uint32_t masked(uint32_t v, uint32_t m) { return v & m; }
 
 // LDS of a workgroup, in this order: borders, every wavefront's slots and table rows of a tile, its maxima and sums, the bias
 // table's columns of the workgroup's heads, and (over the table, once it is done with) the wavefronts' weighted values.
@@ -655,13 +593,8 @@ struct FwdPlan {
     bool even;                 // bags of 512 entries and more in the mean, and not so many that each workgroup could not count them
     uint32_t groups;           // what the chip holds at once
     FwdPlan(const bp_attn* at, int dtype, int64_t n, int64_t bags) {
-        dp = dtype == BP_F32 ? 16 : 32;
-        while (dp < at->head_dim) dp *= 2;
-        // As many heads as have columns, and registers for two workgroups a CU (of four heads of 64, 32 of 1 KB rows: 120 us with
-        // all four in one workgroup, one a CU, 99 with two).
-        pack = 1;
-        const int group = at->q_heads / at->kv_heads;
-        while (pack < at->kv_heads && 2 * pack * group <= 16 && 2 * pack * dp <= 128 && pack < 8) pack *= 2;
+        dp = attn_dp(at, dtype);
+        pack = attn_pack(at, dp);
         chunks = (at->kv_heads + pack - 1) / pack;
         even = bags <= kEvenBags && n >= kLongMean * std::max<int64_t>(bags, 1);
         const int flat = pack * dp;
@@ -689,36 +622,21 @@ struct FwdScratch {
     }
 };
 
-template <typename T, int DP, int PACK>
-int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
-    const int table = f.a.bias ? f.a.rp.rows() * std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads) : 0;
-    const size_t shared = AttnLds<kFwdWaves>::bytes(DP * PACK, table);
-    if (l.even)
-        BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
-    else
-        BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
-    return BP_OK;
-}
-template <typename T, int DP>
-int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
-    switch (l.pack) {
-        case 1: return launch_fwd<T, DP, 1>(f, l, stream);
-        case 2: if constexpr (DP <= 64) return launch_fwd<T, DP, 2>(f, l, stream); break;
-        case 4: if constexpr (DP <= 32) return launch_fwd<T, DP, 4>(f, l, stream); break;
-        case 8: if constexpr (DP <= 16) return launch_fwd<T, DP, 8>(f, l, stream); break;
+struct FwdLaunch {
+    const FwdArgs& f;
+    const FwdPlan& l;
+    hipStream_t stream;
+    template <typename T, int DP, int PACK>
+    int run() {
+        const int table = f.a.bias ? f.a.rp.rows() * std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads) : 0;
+        const size_t shared = AttnLds<kFwdWaves>::bytes(DP * PACK, table);
+        if (l.even)
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+        else
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+        return BP_OK;
     }
-    return fail(BP_ERR_UNSUPPORTED, "no layout for %d heads of %d", l.pack, DP);
-}
-template <typename T>
-int launch_fwd(const FwdArgs& f, const FwdPlan& l, hipStream_t stream) {
-    switch (l.dp) {
-        case 16: if constexpr (sizeof(T) == 4) return launch_fwd<T, 16>(f, l, stream); break;
-        case 32: return launch_fwd<T, 32>(f, l, stream);
-        case 64: return launch_fwd<T, 64>(f, l, stream);
-        case 128: return launch_fwd<T, 128>(f, l, stream);
-    }
-    return launch_fwd<T, 256>(f, l, stream);
-}
+};
 
 }  // namespace
 }  // namespace bp
@@ -765,7 +683,8 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     f.lse = lse;
     f.weight_in = weight_in;
     f.weight_out = weight_out;
-    BP_TRY(cfg->weight_dtype == BP_F32 ? launch_fwd<float>(f, l, stream) : launch_fwd<uint16_t>(f, l, stream));
+    FwdLaunch launch{f, l, stream};
+    BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(l.dp, l.pack, launch) : dispatch_attn<uint16_t>(l.dp, l.pack, launch));
     const bool several = l.even ? l.groups > 1 : n_lookups > (int64_t(1) << f.shift);          // else no bag can have two parts
     if (several) {
         const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
