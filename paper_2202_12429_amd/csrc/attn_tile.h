@@ -83,27 +83,39 @@ inline int attn_pack(const bp_attn* at, int dp) {
     return pack;
 }
 
-// Calls f.template run<T, DP, PACK>() for a layout.
+// Calls f.template run<T, DP, PACK, FULL>() for a layout.  FULL: heads of exactly DP elements, PACK of them in every wavefront, for
+// which the kernels need no test of what lies inside a row (backward, heads of 64: those tests took half of a tile's instructions).
+template <typename T, int DP, int PACK, typename F>
+int dispatch_attn_full(const AttnArgs& a, F&& f) {
+    return a.d == DP && a.kv_heads % PACK == 0 ? f.template run<T, DP, PACK, true>() : f.template run<T, DP, PACK, false>();
+}
 template <typename T, int DP, typename F>
-int dispatch_attn_pack(int pack, F&& f) {
+int dispatch_attn_pack(const AttnArgs& a, int pack, F&& f) {
     switch (pack) {
-        case 1: return f.template run<T, DP, 1>();
-        case 2: if constexpr (DP <= 64) return f.template run<T, DP, 2>(); break;
-        case 4: if constexpr (DP <= 32) return f.template run<T, DP, 4>(); break;
-        case 8: if constexpr (DP <= 16) return f.template run<T, DP, 8>(); break;
+        case 1: return dispatch_attn_full<T, DP, 1>(a, f);
+        case 2: if constexpr (DP <= 64) return dispatch_attn_full<T, DP, 2>(a, f); break;
+        case 4: if constexpr (DP <= 32) return dispatch_attn_full<T, DP, 4>(a, f); break;
+        case 8: if constexpr (DP <= 16) return dispatch_attn_full<T, DP, 8>(a, f); break;
     }
     return fail(BP_ERR_UNSUPPORTED, "no layout for %d heads of %d", pack, DP);
 }
 template <typename T, typename F>
-int dispatch_attn(int dp, int pack, F&& f) {
+int dispatch_attn(const AttnArgs& a, int dp, int pack, F&& f) {
     switch (dp) {
-        case 16: if constexpr (sizeof(T) == 4) return dispatch_attn_pack<T, 16>(pack, f); break;
-        case 32: return dispatch_attn_pack<T, 32>(pack, f);
-        case 64: return dispatch_attn_pack<T, 64>(pack, f);
-        case 128: return dispatch_attn_pack<T, 128>(pack, f);
-        case 256: return dispatch_attn_pack<T, 256>(pack, f);
+        case 16: if constexpr (sizeof(T) == 4) return dispatch_attn_pack<T, 16>(a, pack, f); break;
+        case 32: return dispatch_attn_pack<T, 32>(a, pack, f);
+        case 64: return dispatch_attn_pack<T, 64>(a, pack, f);
+        case 128: return dispatch_attn_pack<T, 128>(a, pack, f);
+        case 256: return dispatch_attn_pack<T, 256>(a, pack, f);
     }
     return fail(BP_ERR_UNSUPPORTED, "no layout for heads of %d", dp);
+}
+
+// 16 bytes of a row, or zeros: the address is one inside the row in any case, so that no load waits for a mask.
+template <bool FULL, typename T>
+__device__ __forceinline__ uint4 row_bytes_at(const T* row, int x, int d) {
+    const uint4 v = *reinterpret_cast<const uint4*>(row + (FULL || x < d ? x : 0));
+    return FULL ? v : masked(v, x < d ? ~0u : 0u);
 }
 
 }  // namespace

@@ -51,7 +51,7 @@ struct BwdLds {
     static size_t floats(int table_rows, int cols) { return 64 + (size_t)kBwdWaves * EACH + (size_t)table_rows * cols + (size_t)kBwdWaves * 4 * table_rows * 16; }
 };
 
-template <typename T, int DP, int PACK>
+template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn_bwd_kernel(BwdArgs f) {
     typedef AttnTile<T, DP, PACK> X;
     typedef BwdLds<T> L;
@@ -61,8 +61,9 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
     extern __shared__ float lds[];
     const AttnArgs& a = f.a;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
-    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = min(PACK, a.kv_heads - kv0);
-    const int first_head = kv0 * group, cols = heads * group, flat = heads * a.d, span = a.kv_heads * a.d;
+    const int d = FULL ? DP : a.d;
+    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0);
+    const int first_head = kv0 * group, cols = heads * group, flat = heads * d, span = a.kv_heads * d;
     const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;
     const int table_rows = a.bias ? a.rp.rows() : 0;
 
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
             hi = min(hi, bag + step);
         }
     }
-    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * a.d;
+    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * d;
     const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
     int sum_row = -1;                                                    // the lane's running sum for the bias table, and its row
     float sum_dz = 0.f;
@@ -108,15 +109,15 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
         const int count = (int)min(s.count - ((int64_t)begin << kUnitShift), (int64_t)(stop - begin) << kUnitShift);
 
         // q and grad_out: for the products with rows, and (a column a quarter) for those with ds and p
-        const float* const q = a.q + ((int64_t)bag * a.q_heads + head) * a.d;
-        const float* const go = f.grad_out + ((int64_t)bag * a.q_heads + head) * a.d;
-        const float* const po = f.out + ((int64_t)bag * a.q_heads + head) * a.d;
+        const float* const q = a.q + ((int64_t)bag * a.q_heads + head) * d;
+        const float* const go = f.grad_out + ((int64_t)bag * a.q_heads + head) * d;
+        const float* const po = f.out + ((int64_t)bag * a.q_heads + head) * d;
         std::conditional_t<X::BF16, Split3, f32x4> qf[X::KM], gf[X::KM];
         float against = 0.f;                                             // <grad_out, out> of the column
 #pragma unroll
         for (int m = 0; m < X::KM; ++m) {
             const int x = m * X::KC + g * (X::KC / 4);
-            const bool have = col < cols && x < a.d;
+            const bool have = col < cols && x < d;
             constexpr int VECS = X::BF16 ? 2 : 1;
             float v[4 * VECS], u[4 * VECS];
 #pragma unroll
@@ -148,8 +149,8 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
 #pragma unroll
                 for (int t = 0; t < STEPS; ++t) {
                     const int c = 4 * t + g, x = 16 * b + col;
-                    const bool have = k < heads && c < group && x < a.d;
-                    const int64_t place = ((int64_t)bag * a.q_heads + first_head + k * group + c) * a.d + x;
+                    const bool have = k < heads && c < group && x < d;
+                    const int64_t place = ((int64_t)bag * a.q_heads + first_head + k * group + c) * d + x;
                     qt[k][b][t] = have ? a.q[place] : 0.f;
                     gt[k][b][t] = have ? f.grad_out[place] : 0.f;
                 }
@@ -166,6 +167,8 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
             if (lane < X::ROWS && e0 + lane < count) slot = a.slots[first + e0 + lane];
             if ((uint32_t)slot < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - a.lookup_pos[first + e0 + lane], borders, a.rp.buckets, a.rp.two_sided) : 0;
             const uint64_t seen = __ballot(row_of >= 0);
+            const int one_row = __builtin_amdgcn_readfirstlane(row_of);
+            const bool same_row = __all(row_of == one_row || lane >= X::ROWS) && one_row >= 0;         // far away, mostly
             const bool all_seen = seen == (X::ROWS == 32 ? 0xffffffffull : 0xffffull);
             __builtin_amdgcn_wave_barrier();
             if (lane < X::ROWS) {
@@ -186,9 +189,9 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
 #pragma unroll
                     for (int m = 0; m < X::KM; ++m) {
                         const int x = m * X::KC + g * (X::KC / 4);
-                        const bool have = x < a.d && k < heads;
-                        kr[k][m] = have ? *reinterpret_cast<const uint4*>(row + k * a.d + x) : make_uint4(0, 0, 0, 0);
-                        vr[k][m] = have ? *reinterpret_cast<const uint4*>(row + a.value_at + k * a.d + x) : make_uint4(0, 0, 0, 0);
+                        const int h = FULL ? k : min(k, heads - 1);                  // (a head that is not there is nobody's)
+                        kr[k][m] = row_bytes_at<FULL>(row + h * d, x, d);
+                        vr[k][m] = row_bytes_at<FULL>(row + a.value_at + h * d, x, d);
                     }
 #pragma unroll
                 for (int k = 0; k < PACK; ++k) {
@@ -224,10 +227,10 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
 #pragma unroll
                 for (int m = 0; m < X::MB; ++m) {
                     const int x = m * 16 * X::VW + col * X::VW;
-                    kv[e][m] = *reinterpret_cast<const VRaw*>(row + (x < flat ? x : 0));
+                    kv[e][m] = *reinterpret_cast<const VRaw*>(row + (FULL || x < flat ? x : 0));
                 }
             }
-            float ds[X::PER];
+            float ds[X::PER], dzs[X::PER];
 #pragma unroll
             for (int e = 0; e < X::PER; ++e) {
                 const int r = tile[32 + X::PER * g + e];
@@ -245,55 +248,85 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
                 ds[e] = dz * bend;
                 turn_ds[(X::PER * g + e) * L::WIDE + col] = ds[e];
                 turn_p[(X::PER * g + e) * L::WIDE + col] = p;
-                if (a.bias && r >= 0 && col < cols) {
+                dzs[e] = dz;
+            }
+            if (a.bias) {
+                const auto turn_to = [&](int r) {
                     if (r != sum_row) {
                         if (sum_row >= 0) sums[sum_row * 16] += sum_dz;
                         sum_row = r;
                         sum_dz = 0.f;
                     }
-                    sum_dz += dz;
+                };
+                if (same_row) {
+                    turn_to(one_row);
+#pragma unroll
+                    for (int e = 0; e < X::PER; ++e) sum_dz += dzs[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < X::PER; ++e) {
+                        const int r = tile[32 + X::PER * g + e];
+                        if (r >= 0) {
+                            turn_to(r);
+                            sum_dz += dzs[e];
+                        }
+                    }
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             // gradients of the rows: elements down (four side by side a lane), entries across
+            const auto row_gradients = [&](auto steps) {
+                constexpr int N = decltype(steps)::value;
 #pragma unroll
-            for (int u = 0; u < X::NU; ++u) {
-                const int entry = 16 * u + col;
-                const bool mine_seen = seen >> entry & 1;
-                float* const to = f.grad_rows + (first + e0 + entry) * a.dim + kv0 * a.d;
+                for (int u = 0; u < X::NU; ++u) {
+                    const int entry = 16 * u + col;
+                    float* const to = f.grad_rows + (first + e0 + entry) * a.dim + kv0 * d + 4 * g;
+                    const bool there = e0 + entry < count, blank = !all_seen && !(seen >> entry & 1);
 #pragma unroll
-                for (int k = 0; k < PACK; ++k) {
-                    float x_ds[STEPS], x_p[STEPS];
+                    for (int k = 0; k < PACK; ++k) {
+                        float x_ds[N], x_p[N];
 #pragma unroll
-                    for (int t = 0; t < STEPS; ++t) {
-                        const bool have = k < heads && 4 * t + g < group;
-                        x_ds[t] = have ? turn_ds[entry * L::WIDE + k * group + 4 * t + g] : 0.f;
-                        x_p[t] = have ? turn_p[entry * L::WIDE + k * group + 4 * t + g] : 0.f;
-                    }
-#pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) {
-                        f32x4 gk = {0.f, 0.f, 0.f, 0.f}, gv = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int t = 0; t < STEPS; ++t) {
-                            if (4 * t >= group) continue;
-                            gk = __builtin_amdgcn_mfma_f32_16x16x4f32(qt[k][b][t], x_ds[t], gk, 0, 0, 0);
-                            gv = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[k][b][t], x_p[t], gv, 0, 0, 0);
+                        for (int t = 0; t < N; ++t) {
+                            const bool have = (FULL || k < heads) && 4 * t + g < group;
+                            const int at_turn = entry * L::WIDE + (have ? k * group + 4 * t + g : 0);
+                            x_ds[t] = have ? turn_ds[at_turn] : 0.f;
+                            x_p[t] = have ? turn_p[at_turn] : 0.f;
                         }
-                        const int x = 16 * b + 4 * g;
-                        if (k < heads && x < a.d && e0 + entry < count) {
-                            if (!mine_seen) gk = gv = f32x4{0.f, 0.f, 0.f, 0.f};
+                        f32x4 gk[BLOCKS], gv[BLOCKS];
+#pragma unroll
+                        for (int b = 0; b < BLOCKS; ++b) {
+                            gk[b] = gv[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int t = 0; t < N; ++t) {
+                                gk[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(qt[k][b][t], x_ds[t], gk[b], 0, 0, 0);
+                                gv[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[k][b][t], x_p[t], gv[b], 0, 0, 0);
+                            }
+                        }
+                        if (!all_seen && blank) {
+#pragma unroll
+                            for (int b = 0; b < BLOCKS; ++b) gk[b] = gv[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        }
+                        if (there && (FULL || k < heads)) {
                             if (a.value_at == 0) {
-                                *reinterpret_cast<f32x4*>(to + k * a.d + x) = gk + gv;
+#pragma unroll
+                                for (int b = 0; b < BLOCKS; ++b)
+                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + k * d + 16 * b) = gk[b] + gv[b];
                             } else {
-                                *reinterpret_cast<f32x4*>(to + k * a.d + x) = gk;
-                                *reinterpret_cast<f32x4*>(to + a.value_at + k * a.d + x) = gv;
+#pragma unroll
+                                for (int b = 0; b < BLOCKS; ++b)
+                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + k * d + 16 * b) = gk[b];
+#pragma unroll
+                                for (int b = 0; b < BLOCKS; ++b)
+                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + a.value_at + k * d + 16 * b) = gv[b];
                             }
                         }
                     }
                 }
-            }
+            };
+            if (STEPS > 1 && group <= 4) row_gradients(std::integral_constant<int, 1>());
+            else row_gradients(std::integral_constant<int, STEPS>());
             // of q: as the forward pass pools values
             if (!all_seen) {
 #pragma unroll
@@ -333,8 +366,8 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
                 const int x = (int)(e % (gap + a.dim - behind));
                 f.grad_rows[(first + e / (gap + a.dim - behind)) * a.dim + (x < gap ? span + x : behind + x - gap)] = 0.f;
             }
-        float* const to = (whole ? f.grad_q + ((int64_t)bag * a.q_heads + head) * a.d
-                                 : f.parts + ((2 * (int64_t)share + starts) * a.q_heads + head) * a.d) - own * a.d;
+        float* const to = (whole ? f.grad_q + ((int64_t)bag * a.q_heads + head) * d
+                                 : f.parts + ((2 * (int64_t)share + starts) * a.q_heads + head) * d) - own * d;
 #pragma unroll
         for (int m = 0; m < X::MB; ++m)
 #pragma unroll
@@ -343,7 +376,7 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
                 float v[X::VW];
 #pragma unroll
                 for (int j = 0; j < X::VW; ++j) v[j] = dq[m][j][i];
-                if (col < cols && x >= own * a.d && x < (own + 1) * a.d) __builtin_memcpy(__builtin_assume_aligned(to + x, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+                if (col < cols && x >= own * d && x < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + x, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
             }
     }
     if (!a.bias) return;
@@ -357,43 +390,46 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
     }
 }
 
-// grad_q of the bags that several wavefronts had a part of: a workgroup 16 elements, four a thread and 64 parts side by side; it
-// looks through `each` bags for such bags.
-constexpr int kJoinBlock = 256, kShare = 16;
+// grad_q of the bags that several wavefronts had a part of.  Workgroups look through `each` bags for such bags.  Up to kFewParts
+// parts: one workgroup, four elements a thread; more: a workgroup 64 elements, 16 parts of them side by side.
+constexpr int kJoinBlock = 256, kShare = 64, kFewParts = 8;
 __global__ __launch_bounds__(kJoinBlock) void embbag_attn_bwd_join_kernel(BwdArgs f, int each) {
-    __shared__ float4 part[kJoinBlock / 64][4];
+    __shared__ float4 part[kJoinBlock];
     const AttnArgs& a = f.a;
-    const int width = a.q_heads * a.d, lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = blockIdx.y * kShare + threadIdx.x % 4 * 4;
+    const int width = a.q_heads * a.d, lane = threadIdx.x % 64;
     const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
     const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
         const uint32_t from = first_unit(a, bag), units = max(1u, (uint32_t)((bag_span(a, bag).count + kUnit - 1) >> kUnitShift));
         *first = share_of(from, f.units, f.waves);
         return share_of(min(from + units, f.units) - 1, f.units, f.waves) - *first + 1;
     };
-    uint32_t first = 0;
-    uint64_t several = __ballot(lane < each && mine < a.bags && parts_of((uint32_t)min(mine, a.bags - 1), &first) > 1);
-    for (; several; several &= several - 1) {
-        const uint32_t bag = (uint32_t)(bag0 + __ffsll((unsigned long long)several) - 1), of = parts_of(bag, &first);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t i = threadIdx.x / 4; i < of && at < width; i += kJoinBlock / 4) {
-            const float4 x = *reinterpret_cast<const float4*>(f.parts + (2 * (int64_t)(first + i) + (i == 0)) * width + at);
-            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-        }
+    uint32_t my_first = 0, my_of = 0;
+    if (lane < each && mine < a.bags) my_of = parts_of((uint32_t)mine, &my_first);
+    const auto add = [](float4& v, const float4& x) { v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w; };
+    for (uint64_t several = __ballot(my_of > 1); several; several &= several - 1) {
+        const int which = __ffsll((unsigned long long)several) - 1;
+        const uint32_t bag = (uint32_t)(bag0 + which), of = __shfl(my_of, which), first = __shfl(my_first, which);
+        const auto from = [&](uint32_t i, int at) { return *reinterpret_cast<const float4*>(f.parts + (2 * (int64_t)(first + i) + (i == 0)) * width + at); };
+        float* const to = f.grad_q + (int64_t)bag * width;
+        if (of <= kFewParts) {
+            if (blockIdx.y > 0) continue;
+            for (int at = 4 * threadIdx.x; at < width; at += 4 * kJoinBlock) {
+                float4 v = from(0, at);
 #pragma unroll
-        for (int off = 4; off < 64; off <<= 1) {
-            v.x += __shfl_xor(v.x, off);
-            v.y += __shfl_xor(v.y, off);
-            v.z += __shfl_xor(v.z, off);
-            v.w += __shfl_xor(v.w, off);
-        }
-        if (lane < 4) part[wave][lane] = v;
-        __syncthreads();
-        if (threadIdx.x < 4 && at < width) {
-            for (int x = 1; x < kJoinBlock / 64; ++x) {
-                const float4 y = part[x][lane];
-                v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+                for (uint32_t i = 1; i < kFewParts; ++i)
+                    if (i < of) add(v, from(i, at));
+                *reinterpret_cast<float4*>(to + at) = v;
             }
-            *reinterpret_cast<float4*>(f.grad_q + (int64_t)bag * width + at) = v;
+            continue;
+        }
+        const int at = blockIdx.y * kShare + threadIdx.x % 16 * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t i = threadIdx.x / 16; i < of && at < width; i += kJoinBlock / 16) add(v, from(i, at));
+        part[threadIdx.x] = v;
+        __syncthreads();
+        if (threadIdx.x < 16 && at < width) {
+            for (int i = 1; i < kJoinBlock / 16; ++i) add(v, part[16 * i + threadIdx.x]);
+            *reinterpret_cast<float4*>(to + at) = v;
         }
         __syncthreads();
     }
@@ -444,11 +480,11 @@ struct BwdLaunch {
     const BwdArgs& f;
     const BwdPlan& l;
     hipStream_t stream;
-    template <typename T, int DP, int PACK>
+    template <typename T, int DP, int PACK, bool FULL>
     int run() {
         const int cols = std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads);
         const size_t shared = BwdLds<T>::floats(f.a.bias ? f.a.rp.rows() : 0, cols) * 4;
-        BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_kernel<T, DP, PACK>), dim3(l.groups, (unsigned)l.chunks), dim3(kBwdBlock), shared, stream, f);
+        BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_kernel<T, DP, PACK, FULL>), dim3(l.groups, (unsigned)l.chunks), dim3(kBwdBlock), shared, stream, f);
         return BP_OK;
     }
 };
@@ -497,7 +533,7 @@ BP_EXPORT int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const 
     f.bias_parts = w.bias_parts;
     if (bags) {
         BwdLaunch launch{f, l, stream};
-        BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(l.dp, l.pack, launch) : dispatch_attn<uint16_t>(l.dp, l.pack, launch));
+        BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(f.a, l.dp, l.pack, launch) : dispatch_attn<uint16_t>(f.a, l.dp, l.pack, launch));
         if (l.waves > 1) {
             const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
             const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);

@@ -135,7 +135,7 @@ struct Segment {
 };
 
 constexpr int kFwdWaves = 4, kFwdBlock = kFwdWaves * 64;
-template <typename T, int DP, int PACK>
+template <typename T, int DP, int PACK, bool FULL>
 __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float* lds) {
     typedef AttnLds<kFwdWaves> L;
     constexpr int kLdsBorders = L::BORDERS, kLdsTile = L::TILE, kLdsMl = L::ML, kLdsFree = L::FREE;
@@ -143,9 +143,9 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
     const AttnArgs& a = f.a;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
-    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = min(PACK, a.kv_heads - kv0);
+    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0), d = FULL ? DP : a.d;
     constexpr int stripes = kFwdWaves;
-    const int stripe = wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * a.d;
+    const int stripe = wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * d;
     const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;        // the column's query head, its kv head
 
     int32_t* const borders = (int32_t*)lds + kLdsBorders;
@@ -173,12 +173,12 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     }
 
     // the queries: lane col has the column's
-    const float* const q = a.q + ((int64_t)p.bag * a.q_heads + head) * a.d;
+    const float* const q = a.q + ((int64_t)p.bag * a.q_heads + head) * d;
     std::conditional_t<X::BF16, Split3, f32x4> qf[X::KM];
 #pragma unroll
     for (int m = 0; m < X::KM; ++m) {
         const int at = m * X::KC + g * (X::KC / 4);
-        const bool have = col < cols && at < a.d;
+        const bool have = col < cols && at < d;
         if constexpr (X::BF16) {
             float v[8];
 #pragma unroll
@@ -200,7 +200,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
         for (int j = 0; j < X::VW; ++j) o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, sum = 0.f;             // of the lane's query head; the sum over the lane's own entries
-    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * a.d;
+    const T* const w = (const T*)a.cache_w + (int64_t)kv0 * d;
 
     // What a tile takes, a step ahead of its use: slots and table offsets into LDS, keys as soon as the tile before has its scores,
     // values as soon as it has pooled, so that one or the other is always on its way, in the registers that it falls free of.
@@ -231,7 +231,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
                 for (int m = 0; m < X::KM; ++m) {
                     const int at = m * X::KC + g * (X::KC / 4);
-                    kraw[k][u][m] = at < a.d && k < heads ? *reinterpret_cast<const uint4*>(row + k * a.d + at) : make_uint4(0, 0, 0, 0);
+                    kraw[k][u][m] = row_bytes_at<FULL>(row + (FULL ? k : min(k, heads - 1)) * d, at, d);      // (a head that is not there is nobody's)
                 }
         }
     };
@@ -244,7 +244,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
             for (int m = 0; m < X::MB; ++m) {
                 const int at = m * 16 * X::VW + col * X::VW;
-                vraw[e][m] = *reinterpret_cast<const VRaw*>(row + (at < flat ? at : 0));
+                vraw[e][m] = *reinterpret_cast<const VRaw*>(row + (FULL || at < flat ? at : 0));
             }
         }
     };
@@ -402,7 +402,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
         }
     }
     // VW elements of the column's head that lie side by side
-    float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * a.d : f.part_o + ((int64_t)p.part * a.q_heads + head) * a.d) - own * a.d;
+    float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * d : f.part_o + ((int64_t)p.part * a.q_heads + head) * d) - own * d;
 #pragma unroll
     for (int m = 0; m < X::MB; ++m) {
         const int at = (m * 16 + 4 * g + wave) * X::VW;
@@ -413,19 +413,19 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
             for (int x = 0; x < kFwdWaves; ++x) v[j] = fmaf(k[x], ox[x * kWaveO + ((m * X::VW + j) * 4 + wave) * 64 + lane], v[j]);
         }
-        if (col < cols && at >= own * a.d && at < (own + 1) * a.d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+        if (col < cols && at >= own * d && at < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
     }
     __syncthreads();                                                 // LDS is free again, the bag's lse there
 }
 
 // A workgroup a piece: calls whose bags are short, or so many that they even out.
-template <typename T, int DP, int PACK>
+template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_fwd_kernel(FwdArgs f) {
     extern __shared__ float lds[];
     const uint32_t id = spread_piece(f.a, f.shift, f.spread, blockIdx.x);
     const BagPiece p = find_piece(f.a, f.shift, id);
     if (p.number >= p.of) return;
-    attend<T, DP, PACK>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
+    attend<T, DP, PACK, FULL>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
     if (f.scores && p.of == 1 && f.weighed) add_weights<kFwdBlock>(f, p.bag, p.first, p.count);       // all heads were this workgroup's
 }
 
@@ -441,7 +441,7 @@ __device__ __forceinline__ uint32_t bag_blocks(const AttnArgs& a, uint32_t bag) 
 __device__ __forceinline__ uint32_t even_start(uint32_t w, uint32_t all, uint32_t groups) { return (uint32_t)((uint64_t)w * all / groups); }
 __device__ __forceinline__ uint32_t even_owner(uint32_t block, uint32_t all, uint32_t groups) { return (uint32_t)(((uint64_t)(block + 1) * groups - 1) / all); }
 
-template <typename T, int DP, int PACK>
+template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_even_kernel(FwdArgs f) {
     extern __shared__ float lds[];
     __shared__ uint32_t wave_sums[kFwdWaves], start_bag, start_block;
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2
         const BagSpan s = bag_span(a, bag);
         const uint32_t mine = max(1u, (uint32_t)((s.count + kBlock - 1) >> kBlockShift)), take = min(mine - block, end - at);
         const int64_t skip = (int64_t)block << kBlockShift;
-        attend<T, DP, PACK>(f, Segment{bag, 2 * blockIdx.x + (block == 0), s.first + skip, (int)min(s.count - skip, (int64_t)take << kBlockShift), take == mine}, lds);
+        attend<T, DP, PACK, FULL>(f, Segment{bag, 2 * blockIdx.x + (block == 0), s.first + skip, (int)min(s.count - skip, (int64_t)take << kBlockShift), take == mine}, lds);
         at += take;
         block = 0;
         ++bag;
@@ -626,14 +626,14 @@ struct FwdLaunch {
     const FwdArgs& f;
     const FwdPlan& l;
     hipStream_t stream;
-    template <typename T, int DP, int PACK>
+    template <typename T, int DP, int PACK, bool FULL>
     int run() {
         const int table = f.a.bias ? f.a.rp.rows() * std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads) : 0;
         const size_t shared = AttnLds<kFwdWaves>::bytes(DP * PACK, table);
         if (l.even)
-            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK, FULL>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
         else
-            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK, FULL>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
         return BP_OK;
     }
 };
@@ -684,7 +684,7 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     f.weight_in = weight_in;
     f.weight_out = weight_out;
     FwdLaunch launch{f, l, stream};
-    BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(l.dp, l.pack, launch) : dispatch_attn<uint16_t>(l.dp, l.pack, launch));
+    BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(f.a, l.dp, l.pack, launch) : dispatch_attn<uint16_t>(f.a, l.dp, l.pack, launch));
     const bool several = l.even ? l.groups > 1 : n_lookups > (int64_t(1) << f.shift);          // else no bag can have two parts
     if (several) {
         const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
