@@ -42,12 +42,12 @@ __device__ __forceinline__ uint32_t share_of(uint32_t unit, uint32_t units, uint
     return min((uint32_t)(((uint64_t)(unit + 1) * waves - 1) / units), waves - 1);
 }
 
-// LDS: borders, the bias table's columns of the workgroup's heads; of every wavefront a tile's slots and table offsets, its ds and p
+// LDS: borders, the bias table's columns of the workgroup's heads; of every wavefront two tiles' slots and table rows, a tile's ds and p
 // entry by entry, and four tables of sums, one for each quarter of the wavefront, in which a column is one lane's.
 template <typename T>
 struct BwdLds {
     static constexpr int ROWS = sizeof(T) == 2 ? 32 : 16, WIDE = 17;
-    static constexpr int TILE = 64, TURN = TILE + 64, EACH = 64 + 2 * ROWS * WIDE;      // of a wavefront behind the borders
+    static constexpr int EACH = 128 + 2 * ROWS * WIDE;                                  // of a wavefront behind the borders
     static size_t floats(int table_rows, int cols) { return 64 + (size_t)kBwdWaves * EACH + (size_t)table_rows * cols + (size_t)kBwdWaves * 4 * table_rows * 16; }
 };
 
@@ -68,8 +68,8 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
     const int table_rows = a.bias ? a.rp.rows() : 0;
 
     int32_t* const borders = (int32_t*)lds;
-    int32_t* const tile = (int32_t*)lds + 64 + wave * L::EACH;           // slots, then table offsets
-    float* const turn_ds = lds + 64 + wave * L::EACH + 64;               // [entry][column]
+    int32_t* const tiles_of = (int32_t*)lds + 64 + wave * L::EACH;       // two tiles: slots, then table rows
+    float* const turn_ds = lds + 64 + wave * L::EACH + 128;              // [entry][column]
     float* const turn_p = turn_ds + L::ROWS * L::WIDE;
     float* const table = lds + 64 + kBwdWaves * L::EACH;
     float* const sums = table + table_rows * cols + wave * 4 * table_rows * 16 + g * table_rows * 16 + col;      // this lane's column
@@ -162,63 +162,56 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
 #pragma unroll
             for (int j = 0; j < X::VW; ++j) dq[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        for (int e0 = 0; e0 < count; e0 += X::ROWS) {
-            int row_of = -1, slot = -1;
-            if (lane < X::ROWS && e0 + lane < count) slot = a.slots[first + e0 + lane];
-            if ((uint32_t)slot < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - a.lookup_pos[first + e0 + lane], borders, a.rp.buckets, a.rp.two_sided) : 0;
-            const uint64_t seen = __ballot(row_of >= 0);
-            const int one_row = __builtin_amdgcn_readfirstlane(row_of);
-            const bool same_row = __all(row_of == one_row || lane >= X::ROWS) && one_row >= 0;         // far away, mostly
-            const bool all_seen = seen == (X::ROWS == 32 ? 0xffffffffull : 0xffffull);
+        // A tile's slots come two tiles ahead of their rows' use, its rows as soon as the tile before has its scores.
+        int32_t slot_n = -1, pos_n = 0;
+        const auto fetch = [&](int e0) {
+            const bool have = lane < X::ROWS && e0 + lane < count;
+            slot_n = have ? a.slots[first + e0 + lane] : -1;
+            pos_n = have && a.bias ? a.lookup_pos[first + e0 + lane] : 0;
+        };
+        uint64_t seen_n = 0;
+        int one_row_n = -1;                                              // the table row, where all entries have the same: far away, mostly
+        const auto place = [&](int e0) {
+            int row_of = -1;
+            if ((uint32_t)slot_n < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - pos_n, borders, a.rp.buckets, a.rp.two_sided) : 0;
+            seen_n = __ballot(row_of >= 0);
+            const int one = __builtin_amdgcn_readfirstlane(row_of);
+            one_row_n = __all(row_of == one || lane >= X::ROWS) ? one : -1;
+            int32_t* const tile = tiles_of + (e0 / X::ROWS & 1) * 64;
             __builtin_amdgcn_wave_barrier();
             if (lane < X::ROWS) {
-                tile[lane] = row_of >= 0 ? slot : 0;                     // what is not seen reads row 0, and leaves it out
+                tile[lane] = row_of >= 0 ? slot_n : 0;                   // what is not seen reads row 0, and leaves it out
                 tile[32 + lane] = row_of;
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            // scores and <grad_out, value>, each entry's against every column
-            float c[X::PER], dp[X::PER];
+        };
+        uint4 kr[X::NU][PACK][X::KM], vr[X::NU][PACK][X::KM];
+        const auto load_rows = [&](int e0) {
+            const int32_t* const tile = tiles_of + (e0 / X::ROWS & 1) * 64;
 #pragma unroll
             for (int u = 0; u < X::NU; ++u) {
                 const T* const row = w + (int64_t)tile[X::PER * (col / 4) + 4 * u + col % 4] * a.wst;
-                uint4 kr[PACK][X::KM], vr[PACK][X::KM];
 #pragma unroll
                 for (int k = 0; k < PACK; ++k)
 #pragma unroll
                     for (int m = 0; m < X::KM; ++m) {
-                        const int x = m * X::KC + g * (X::KC / 4);
-                        const int h = FULL ? k : min(k, heads - 1);                  // (a head that is not there is nobody's)
-                        kr[k][m] = row_bytes_at<FULL>(row + h * d, x, d);
-                        vr[k][m] = row_bytes_at<FULL>(row + a.value_at + h * d, x, d);
+                        const int x = m * X::KC + g * (X::KC / 4), h = FULL ? k : min(k, heads - 1);      // (a head that is not there is nobody's)
+                        kr[u][k][m] = row_bytes_at<FULL>(row + h * d, x, d);
+                        vr[u][k][m] = row_bytes_at<FULL>(row + a.value_at + h * d, x, d);
                     }
-#pragma unroll
-                for (int k = 0; k < PACK; ++k) {
-                    f32x4 sc = {0.f, 0.f, 0.f, 0.f}, sp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int m = 0; m < X::KM; ++m) {
-                        if constexpr (X::BF16) {
-#pragma unroll
-                            for (int part = 2; part >= 0; --part) {
-                                sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[k][m]), qf[m].part[part], sc, 0, 0, 0);
-                                sp = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[k][m]), gf[m].part[part], sp, 0, 0, 0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kr[k][m], i)), qf[m][i], sc, 0, 0, 0);
-                                sp = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vr[k][m], i)), gf[m][i], sp, 0, 0, 0);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        c[4 * u + i] = k == 0 || own == k ? sc[i] : c[4 * u + i];
-                        dp[4 * u + i] = k == 0 || own == k ? sp[i] : dp[4 * u + i];
-                    }
-                }
             }
+        };
+        fetch(0);
+        place(0);
+        load_rows(0);
+        fetch(X::ROWS);
+        for (int e0 = 0; e0 < count; e0 += X::ROWS) {
+            const int32_t* const tile = tiles_of + (e0 / X::ROWS & 1) * 64;
+            const uint64_t seen = seen_n;
+            const int one_row = one_row_n;
+            const bool all_seen = seen == (X::ROWS == 32 ? 0xffffffffull : 0xffffull);
             // the keys again, in whole rows (from the caches)
             VRaw kv[X::PER][X::MB];
 #pragma unroll
@@ -229,6 +222,40 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
                     const int x = m * 16 * X::VW + col * X::VW;
                     kv[e][m] = *reinterpret_cast<const VRaw*>(row + (FULL || x < flat ? x : 0));
                 }
+            }
+            // scores and <grad_out, value>, each entry's against every column
+            float c[X::PER], dp[X::PER];
+#pragma unroll
+            for (int u = 0; u < X::NU; ++u)
+#pragma unroll
+                for (int k = 0; k < PACK; ++k) {
+                    f32x4 sc = {0.f, 0.f, 0.f, 0.f}, sp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int m = 0; m < X::KM; ++m) {
+                        if constexpr (X::BF16) {
+#pragma unroll
+                            for (int part = 2; part >= 0; --part) {
+                                sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[u][k][m]), qf[m].part[part], sc, 0, 0, 0);
+                                sp = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[u][k][m]), gf[m].part[part], sp, 0, 0, 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kr[u][k][m], i)), qf[m][i], sc, 0, 0, 0);
+                                sp = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vr[u][k][m], i)), gf[m][i], sp, 0, 0, 0);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        c[4 * u + i] = k == 0 || own == k ? sc[i] : c[4 * u + i];
+                        dp[4 * u + i] = k == 0 || own == k ? sp[i] : dp[4 * u + i];
+                    }
+                }
+            if (e0 + X::ROWS < count) {
+                place(e0 + X::ROWS);
+                load_rows(e0 + X::ROWS);
+                fetch(e0 + 2 * X::ROWS);
             }
             float ds[X::PER], dzs[X::PER];
 #pragma unroll
@@ -258,7 +285,7 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
                         sum_dz = 0.f;
                     }
                 };
-                if (same_row) {
+                if (one_row >= 0) {
                     turn_to(one_row);
 #pragma unroll
                     for (int e = 0; e < X::PER; ++e) sum_dz += dzs[e];
