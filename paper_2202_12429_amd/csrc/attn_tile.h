@@ -111,6 +111,10 @@ int dispatch_attn(const AttnArgs& a, int dp, int pack, F&& f) {
     return fail(BP_ERR_UNSUPPORTED, "no layout for heads of %d", dp);
 }
 
+__device__ __forceinline__ float4 or_zeros(const float4& v, bool have) {
+    return make_float4(have ? v.x : 0.f, have ? v.y : 0.f, have ? v.z : 0.f, have ? v.w : 0.f);
+}
+
 // 16 bytes of a row, or zeros: the address is one inside the row in any case, so that no load waits for a mask.
 template <bool FULL, typename T>
 __device__ __forceinline__ uint4 row_bytes_at(const T* row, int x, int d) {

@@ -44,23 +44,32 @@ __device__ __forceinline__ uint32_t share_of(uint32_t unit, uint32_t units, uint
 
 // LDS: borders, the bias table's columns of the workgroup's heads; of every wavefront two tiles' slots and table rows, a tile's ds and p
 // entry by entry, and four tables of sums, one for each quarter of the wavefront, in which a column is one lane's.
-template <typename T>
+// STAGE: 16 entries' row gradients, to be written out a row at a time: keys' and values', or, of wide heads, a stretch of either.
+template <typename T, int DP, int PACK, bool FULL>
 struct BwdLds {
-    static constexpr int ROWS = sizeof(T) == 2 ? 32 : 16, WIDE = 17;
-    static constexpr int EACH = 128 + 2 * ROWS * WIDE;                                  // of a wavefront behind the borders
+    static constexpr int FLAT = DP * PACK, ROWS = sizeof(T) == 2 ? 32 : 16, WIDE = 17;
+    static constexpr bool STAGED = FULL, APART = DP > 64;
+    static constexpr int STRETCH = APART ? 128 : FLAT, STAGE_WIDE = (APART ? 1 : 2) * STRETCH + 4, STAGE = STAGED ? 16 * STAGE_WIDE : 0;
+    static constexpr int EACH = 128 + 2 * ROWS * WIDE + STAGE;                          // of a wavefront behind the borders
     static size_t floats(int table_rows, int cols) { return 64 + (size_t)kBwdWaves * EACH + (size_t)table_rows * cols + (size_t)kBwdWaves * 4 * table_rows * 16; }
 };
 
+// Workgroups that a CU holds, by their registers.
+constexpr int bwd_groups_a_cu(size_t elem, int dp, int flat) { return flat <= 32 || (elem == 4 && dp <= 32 && flat <= 64) ? 2 : 1; }
+
 template <typename T, int DP, int PACK, bool FULL>
-__global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn_bwd_kernel(BwdArgs f) {
+__global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK)) void embbag_attn_bwd_kernel(BwdArgs f) {
     typedef AttnTile<T, DP, PACK> X;
-    typedef BwdLds<T> L;
+    typedef BwdLds<T, DP, PACK, FULL> L;
     typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
     constexpr int STEPS = PACK == 1 ? 4 : PACK == 2 ? 2 : 1;             // of four columns, in a head's group
-    constexpr int BLOCKS = DP / 16;                                      // of 16 elements of a head
+    constexpr int BLOCKS = DP / 16, SOME = BLOCKS < 8 ? BLOCKS : 8;      // of 16 elements of a head; blocks whose gradients are in work at a time
+    // q and grad_out in registers all along a bag, where they fit; else from the caches, tile by tile (400,000 rows of 2 x 256 bf16: 430 us so,
+    // 1370 with registers spilled)
+    constexpr bool KEEP = DP <= 128;
     extern __shared__ float lds[];
     const AttnArgs& a = f.a;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     const int d = FULL ? DP : a.d;
     const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0);
     const int first_head = kv0 * group, cols = heads * group, flat = heads * d, span = a.kv_heads * d;
@@ -71,6 +80,7 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
     int32_t* const tiles_of = (int32_t*)lds + 64 + wave * L::EACH;       // two tiles: slots, then table rows
     float* const turn_ds = lds + 64 + wave * L::EACH + 128;              // [entry][column]
     float* const turn_p = turn_ds + L::ROWS * L::WIDE;
+    float* const stage = turn_p + L::ROWS * L::WIDE;                     // [entry][key, value][element]
     float* const table = lds + 64 + kBwdWaves * L::EACH;
     float* const sums = table + table_rows * cols + wave * 4 * table_rows * 16 + g * table_rows * 16 + col;      // this lane's column
     if (a.bias) {
@@ -112,48 +122,57 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
         const float* const q = a.q + ((int64_t)bag * a.q_heads + head) * d;
         const float* const go = f.grad_out + ((int64_t)bag * a.q_heads + head) * d;
         const float* const po = f.out + ((int64_t)bag * a.q_heads + head) * d;
-        std::conditional_t<X::BF16, Split3, f32x4> qf[X::KM], gf[X::KM];
+        typedef std::conditional_t<X::BF16, Split3, f32x4> Frag;
+        const auto columns = [&](const float* of, int m, float (&v)[X::KC / 4]) {       // elements of the column's head that are this lane's
+            const int x = m * X::KC + g * (X::KC / 4);
+#pragma unroll
+            for (int i = 0; i < X::KC / 16; ++i) {
+                const int place = (FULL || x < d ? x : 0) + 4 * i;       // inside the row in any case, as below: no branch a load
+                const float4 t = or_zeros(*reinterpret_cast<const float4*>(of + place), col < cols && x < d);
+                v[4 * i] = t.x, v[4 * i + 1] = t.y, v[4 * i + 2] = t.z, v[4 * i + 3] = t.w;
+            }
+        };
+        const auto fragment = [&](Frag& to, const float (&v)[X::KC / 4]) {
+            if constexpr (X::BF16) to.set(v);
+            else to = f32x4{v[0], v[1], v[2], v[3]};
+        };
+        Frag qf[KEEP ? X::KM : 1], gf[KEEP ? X::KM : 1];
         float against = 0.f;                                             // <grad_out, out> of the column
 #pragma unroll
         for (int m = 0; m < X::KM; ++m) {
-            const int x = m * X::KC + g * (X::KC / 4);
-            const bool have = col < cols && x < d;
-            constexpr int VECS = X::BF16 ? 2 : 1;
-            float v[4 * VECS], u[4 * VECS];
+            float u[X::KC / 4], o[X::KC / 4];
+            columns(go, m, u);
+            columns(po, m, o);
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) {
-                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-                const float4 tq = have ? *reinterpret_cast<const float4*>(q + x + 4 * i) : zero;
-                const float4 tg = have ? *reinterpret_cast<const float4*>(go + x + 4 * i) : zero;
-                const float4 to = have ? *reinterpret_cast<const float4*>(po + x + 4 * i) : zero;
-                v[4 * i] = tq.x, v[4 * i + 1] = tq.y, v[4 * i + 2] = tq.z, v[4 * i + 3] = tq.w;
-                u[4 * i] = tg.x, u[4 * i + 1] = tg.y, u[4 * i + 2] = tg.z, u[4 * i + 3] = tg.w;
-                against = fmaf(tg.x, to.x, fmaf(tg.y, to.y, fmaf(tg.z, to.z, fmaf(tg.w, to.w, against))));
-            }
-            if constexpr (X::BF16) {
-                qf[m].set(v);
-                gf[m].set(u);
-            } else {
-                qf[m] = f32x4{v[0], v[1], v[2], v[3]};
-                gf[m] = f32x4{u[0], u[1], u[2], u[3]};
+            for (int i = 0; i < X::KC / 4; ++i) against = fmaf(u[i], o[i], against);
+            if constexpr (KEEP) {
+                float v[X::KC / 4];
+                columns(q, m, v);
+                fragment(qf[m], v);
+                fragment(gf[m], u);
             }
         }
         against += __shfl_xor(against, 16);
         against += __shfl_xor(against, 32);
         const float lse = f.lse[(int64_t)bag * a.q_heads + head];
-        float qt[PACK][BLOCKS][STEPS], gt[PACK][BLOCKS][STEPS];          // element 16 * block + col of head k's column 4 * step + g
+        const auto element = [&](const float* of, int k, int b, int t) { // 16 * block + col of head k's column 4 * step + g
+            const int c = 4 * t + g, x = 16 * b + col;
+            const int64_t place = ((int64_t)bag * a.q_heads + first_head + (FULL ? k : min(k, heads - 1)) * group + min(c, group - 1)) * d + (FULL ? x : min(x, d - 1));
+            const float v = of[place];
+            return k < heads && c < group && x < d ? v : 0.f;
+        };
+        float qt[KEEP ? PACK : 1][BLOCKS][STEPS], gt[KEEP ? PACK : 1][BLOCKS][STEPS];
+        if constexpr (KEEP) {
 #pragma unroll
-        for (int k = 0; k < PACK; ++k)
+            for (int k = 0; k < PACK; ++k)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
+                for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    const int c = 4 * t + g, x = 16 * b + col;
-                    const bool have = k < heads && c < group && x < d;
-                    const int64_t place = ((int64_t)bag * a.q_heads + first_head + k * group + c) * d + x;
-                    qt[k][b][t] = have ? a.q[place] : 0.f;
-                    gt[k][b][t] = have ? f.grad_out[place] : 0.f;
-                }
+                    for (int t = 0; t < STEPS; ++t) {
+                        qt[k][b][t] = element(a.q, k, b, t);
+                        gt[k][b][t] = element(f.grad_out, k, b, t);
+                    }
+        }
         const int64_t q_pos = a.bias ? a.q_pos[bag] : 0;
 
         f32x4 dq[X::MB][X::VW];
@@ -187,19 +206,23 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         };
+        const auto row_of_tile = [&](int e0, int u) {
+            return w + (int64_t)(tiles_of + (e0 / X::ROWS & 1) * 64)[X::PER * (col / 4) + 4 * u + col % 4] * a.wst;
+        };
+        const auto row_part = [&](const T* row, int k, int m) {          // (a head that is not there is nobody's)
+            return row_bytes_at<FULL>(row + (FULL ? k : min(k, heads - 1)) * d, m * X::KC + g * (X::KC / 4), d);
+        };
         uint4 kr[X::NU][PACK][X::KM], vr[X::NU][PACK][X::KM];
         const auto load_rows = [&](int e0) {
-            const int32_t* const tile = tiles_of + (e0 / X::ROWS & 1) * 64;
 #pragma unroll
             for (int u = 0; u < X::NU; ++u) {
-                const T* const row = w + (int64_t)tile[X::PER * (col / 4) + 4 * u + col % 4] * a.wst;
+                const T* const row = row_of_tile(e0, u);
 #pragma unroll
                 for (int k = 0; k < PACK; ++k)
 #pragma unroll
                     for (int m = 0; m < X::KM; ++m) {
-                        const int x = m * X::KC + g * (X::KC / 4), h = FULL ? k : min(k, heads - 1);      // (a head that is not there is nobody's)
-                        kr[u][k][m] = row_bytes_at<FULL>(row + h * d, x, d);
-                        vr[u][k][m] = row_bytes_at<FULL>(row + a.value_at + h * d, x, d);
+                        kr[u][k][m] = row_part(row, k, m);
+                        vr[u][k][m] = row_part(row + a.value_at, k, m);
                     }
             }
         };
@@ -214,65 +237,107 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
             const bool all_seen = seen == (X::ROWS == 32 ? 0xffffffffull : 0xffffull);
             // the keys again, in whole rows (from the caches)
             VRaw kv[X::PER][X::MB];
+            const auto whole_keys = [&]() {
 #pragma unroll
-            for (int e = 0; e < X::PER; ++e) {
-                const T* const row = w + (int64_t)tile[X::PER * g + e] * a.wst;
+                for (int e = 0; e < X::PER; ++e) {
+                    const T* const row = w + (int64_t)tile[X::PER * g + e] * a.wst;
 #pragma unroll
-                for (int m = 0; m < X::MB; ++m) {
-                    const int x = m * 16 * X::VW + col * X::VW;
-                    kv[e][m] = *reinterpret_cast<const VRaw*>(row + (FULL || x < flat ? x : 0));
+                    for (int m = 0; m < X::MB; ++m) {
+                        const int x = m * 16 * X::VW + col * X::VW;
+                        kv[e][m] = *reinterpret_cast<const VRaw*>(row + (FULL || x < flat ? x : 0));
+                    }
                 }
-            }
+            };
+            whole_keys();
             // scores and <grad_out, value>, each entry's against every column
+            const auto product = [&](const uint4& rows, const Frag& with, f32x4& sum) {
+                if constexpr (X::BF16) {
+#pragma unroll
+                    for (int part = 2; part >= 0; --part)
+                        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows), with.part[part], sum, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(rows, i)), with[i], sum, 0, 0, 0);
+                }
+            };
             float c[X::PER], dp[X::PER];
+            if constexpr (KEEP) {
 #pragma unroll
-            for (int u = 0; u < X::NU; ++u)
+                for (int u = 0; u < X::NU; ++u)
 #pragma unroll
-                for (int k = 0; k < PACK; ++k) {
-                    f32x4 sc = {0.f, 0.f, 0.f, 0.f}, sp = {0.f, 0.f, 0.f, 0.f};
+                    for (int k = 0; k < PACK; ++k) {
+                        f32x4 sc = {0.f, 0.f, 0.f, 0.f}, sp = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int m = 0; m < X::KM; ++m) {
-                        if constexpr (X::BF16) {
+                        for (int m = 0; m < X::KM; ++m) {
+                            product(kr[u][k][m], qf[m], sc);
+                            product(vr[u][k][m], gf[m], sp);
+                        }
 #pragma unroll
-                            for (int part = 2; part >= 0; --part) {
-                                sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[u][k][m]), qf[m].part[part], sc, 0, 0, 0);
-                                sp = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[u][k][m]), gf[m].part[part], sp, 0, 0, 0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kr[u][k][m], i)), qf[m][i], sc, 0, 0, 0);
-                                sp = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vr[u][k][m], i)), gf[m][i], sp, 0, 0, 0);
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            c[4 * u + i] = k == 0 || own == k ? sc[i] : c[4 * u + i];
+                            dp[4 * u + i] = k == 0 || own == k ? sp[i] : dp[4 * u + i];
                         }
                     }
+            } else {                                                     // (heads this wide are alone in their wavefront)
+                f32x4 sc[X::NU], sp[X::NU];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        c[4 * u + i] = k == 0 || own == k ? sc[i] : c[4 * u + i];
-                        dp[4 * u + i] = k == 0 || own == k ? sp[i] : dp[4 * u + i];
+                for (int u = 0; u < X::NU; ++u) sc[u] = sp[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int m0 = 0; m0 < X::KM; m0 += 2) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    float v[2][X::KC / 4], o[2][X::KC / 4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        columns(q, m0 + h, v[h]);
+                        columns(go, m0 + h, o[h]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        fragment(qf[0], v[h]);
+                        fragment(gf[0], o[h]);
+#pragma unroll
+                        for (int u = 0; u < X::NU; ++u) {
+                            product(kr[u][0][m0 + h], qf[0], sc[u]);
+                            product(vr[u][0][m0 + h], gf[0], sp[u]);
+                        }
                     }
                 }
+#pragma unroll
+                for (int u = 0; u < X::NU; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[4 * u + i] = sc[u][i], dp[4 * u + i] = sp[u][i];
+            }
             if (e0 + X::ROWS < count) {
                 place(e0 + X::ROWS);
                 load_rows(e0 + X::ROWS);
                 fetch(e0 + 2 * X::ROWS);
             }
-            float ds[X::PER], dzs[X::PER];
+            float z[X::PER], bend[X::PER], ds[X::PER], dzs[X::PER];
+            if (a.cap > 0) {                                             // (tests of what the call has stay outside the loops over entries)
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e) {
+                    const float t = tanh_few_ulp(c[e] * by_cap);
+                    z[e] = a.cap * t;
+                    bend[e] = a.scale * fmaf(-t, t, 1.f);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e) {
+                    z[e] = c[e] * a.scale;
+                    bend[e] = a.scale;
+                }
+            }
+            if (a.bias) {
+#pragma unroll
+                for (int e = 0; e < X::PER; ++e) z[e] += table[max(tile[32 + X::PER * g + e], 0) * cols + min(col, cols - 1)];
+            }
 #pragma unroll
             for (int e = 0; e < X::PER; ++e) {
-                const int r = tile[32 + X::PER * g + e];
-                float z = c[e] * a.scale, bend = a.scale;
-                if (a.cap > 0) {
-                    const float t = tanh_few_ulp(c[e] * by_cap);
-                    z = a.cap * t;
-                    bend *= fmaf(-t, t, 1.f);
-                }
-                if (a.bias) z += table[max(r, 0) * cols + min(col, cols - 1)];
-                const bool in = r >= 0 && z != -INFINITY;                // (a score of -infinity weighs nothing, also in a bag of them alone)
+                const bool in = (seen >> (X::PER * g + e) & 1) && z[e] != -INFINITY;      // (a score of -infinity weighs nothing, also in a bag of them alone)
                 // A weight that rounds to 1 has all others below a rounding, and its score no gradient but the two products' difference in
                 // rounding, which a step of Adagrad would blow up (bags of one entry).
-                const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in && p != 1.f ? p * (dp[e] - against) : 0.f;
-                ds[e] = dz * bend;
+                const float p = in ? exp_few_ulp(z[e] - lse) : 0.f, dz = in && p != 1.f ? p * (dp[e] - against) : 0.f;
+                ds[e] = dz * bend[e];
                 turn_ds[(X::PER * g + e) * L::WIDE + col] = ds[e];
                 turn_p[(X::PER * g + e) * L::WIDE + col] = p;
                 dzs[e] = dz;
@@ -303,53 +368,135 @@ __global__ __launch_bounds__(kBwdBlock, DP * PACK > 64 ? 1 : 2) void embbag_attn
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            // gradients of the rows: elements down (four side by side a lane), entries across
+            // Gradients of the rows: elements down (four side by side a lane), entries across.  Straight from the registers a store would
+            // write 64 bytes of 16 rows each, which memory takes at half the rate of whole rows (400,000 rows of 1 KB: 161 us so, 140 this).
             const auto row_gradients = [&](auto steps) {
                 constexpr int N = decltype(steps)::value;
+                // a head's gradients of the keys or of the values, added to `to`: from its columns' elements and what the entries have of them
+                const auto of_head = [&](const float (&y)[SOME][STEPS], const float* turn, int u, int k, f32x4 (&to)[SOME]) {
+                    float x[N];
 #pragma unroll
-                for (int u = 0; u < X::NU; ++u) {
+                    for (int t = 0; t < N; ++t) {
+                        const bool have = (FULL || k < heads) && 4 * t + g < group;
+                        const float v = turn[(16 * u + col) * L::WIDE + (have ? k * group + 4 * t + g : 0)];
+                        x[t] = have ? v : 0.f;
+                    }
+#pragma unroll
+                    for (int b = 0; b < SOME; ++b)
+#pragma unroll
+                        for (int t = 0; t < N; ++t) to[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[b][t], x[t], to[b], 0, 0, 0);
+                };
+                const auto with_rows = [&](int u, auto&& then) {
                     const int entry = 16 * u + col;
-                    float* const to = f.grad_rows + (first + e0 + entry) * a.dim + kv0 * d + 4 * g;
-                    const bool there = e0 + entry < count, blank = !all_seen && !(seen >> entry & 1);
+                    float* const rows_at = f.grad_rows + (first + e0 + 16 * u) * a.dim + kv0 * d;
+                    const bool blank = !all_seen && !(seen >> entry & 1);
+                    const auto zero = [&](f32x4 (&to)[SOME]) {
 #pragma unroll
-                    for (int k = 0; k < PACK; ++k) {
-                        float x_ds[N], x_p[N];
+                        for (int b = 0; b < SOME; ++b) to[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    };
+                    const auto to_stage = [&](const f32x4 (&from)[SOME], int at) {
 #pragma unroll
-                        for (int t = 0; t < N; ++t) {
-                            const bool have = (FULL || k < heads) && 4 * t + g < group;
-                            const int at_turn = entry * L::WIDE + (have ? k * group + 4 * t + g : 0);
-                            x_ds[t] = have ? turn_ds[at_turn] : 0.f;
-                            x_p[t] = have ? turn_p[at_turn] : 0.f;
+                        for (int b = 0; b < SOME; ++b) *reinterpret_cast<f32x4*>(stage + col * L::STAGE_WIDE + at + 16 * b + 4 * g) = from[b];
+                    };
+                    const auto to_rows = [&](const f32x4 (&from)[SOME], int at, int b0) {
+                        if (e0 + entry >= count) return;
+#pragma unroll
+                        for (int b = 0; b < SOME; ++b)
+                            if (FULL || 16 * (b0 + b) + 4 * g < d) *reinterpret_cast<f32x4*>(rows_at + (int64_t)col * a.dim + at + 16 * b + 4 * g) = from[b];
+                    };
+                    const auto write_rows = [&](auto parts, int at) {
+                        constexpr int UNITS = L::STRETCH / 4, EVERY = decltype(parts)::value * UNITS, ROWS_A_TIME = 64 / EVERY, TIMES = 16 / ROWS_A_TIME;      // units of 16 bytes
+                        constexpr int AHEAD = TIMES < 4 ? TIMES : 4;
+                        static_assert(EVERY <= 64);
+                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                        const int my_row = lane / EVERY, part = lane % EVERY / UNITS, unit = lane % UNITS, left = count - e0 - 16 * u - my_row;
+                        const uint32_t lane_at = my_row * a.dim + part * a.value_at + 4 * unit;
+                        const float* const from = stage + my_row * L::STAGE_WIDE + part * L::STRETCH + 4 * unit;
+#pragma unroll
+                        for (int i0 = 0; i0 < TIMES; i0 += AHEAD) {
+                            f32x4 v[AHEAD];
+#pragma unroll
+                            for (int j = 0; j < AHEAD; ++j) v[j] = *reinterpret_cast<const f32x4*>(from + (i0 + j) * ROWS_A_TIME * L::STAGE_WIDE);
+#pragma unroll
+                            for (int j = 0; j < AHEAD; ++j)
+                                if ((i0 + j) * ROWS_A_TIME < left) *reinterpret_cast<f32x4*>(rows_at + at + (int64_t)((i0 + j) * ROWS_A_TIME) * a.dim + lane_at) = v[j];
                         }
-                        f32x4 gk[BLOCKS], gv[BLOCKS];
+                        __builtin_amdgcn_wave_barrier();
+                    };
+                    then(blank, zero, to_stage, to_rows, write_rows);
+                };
+                const std::integral_constant<int, 1> one;
+                if constexpr (L::APART) {
+                    const auto of_part = [&](const float (&y)[SOME][STEPS], const float (&also)[SOME][STEPS], bool values, int b0) {
 #pragma unroll
-                        for (int b = 0; b < BLOCKS; ++b) {
-                            gk[b] = gv[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int u = 0; u < X::NU; ++u)
+                            with_rows(u, [&](bool blank, auto zero, auto to_stage, auto to_rows, auto write_rows) {
+                                f32x4 of[SOME];
+                                zero(of);
+                                of_head(y, values ? turn_p : turn_ds, u, 0, of);
+                                if (a.value_at == 0) of_head(also, turn_p, u, 0, of);
+                                if (blank) zero(of);
+                                if constexpr (L::STAGED) {
+                                    to_stage(of, 0);
+                                    write_rows(one, (values ? a.value_at : 0) + 16 * b0);
+                                } else {
+                                    to_rows(of, (values ? a.value_at : 0) + 16 * b0, b0);
+                                }
+                            });
+                    };
+                    if constexpr (KEEP) {
+                        of_part(qt[0], gt[0], false, 0);
+                        if (a.value_at) of_part(gt[0], gt[0], true, 0);
+                    } else {
+#pragma unroll 1
+                        for (int b0 = 0; b0 < BLOCKS; b0 += SOME) {
+                            float y[SOME][STEPS], also[SOME][STEPS];
 #pragma unroll
-                            for (int t = 0; t < N; ++t) {
-                                gk[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(qt[k][b][t], x_ds[t], gk[b], 0, 0, 0);
-                                gv[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[k][b][t], x_p[t], gv[b], 0, 0, 0);
-                            }
-                        }
-                        if (!all_seen && blank) {
+                            for (int b = 0; b < SOME; ++b)
 #pragma unroll
-                            for (int b = 0; b < BLOCKS; ++b) gk[b] = gv[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        }
-                        if (there && (FULL || k < heads)) {
-                            if (a.value_at == 0) {
-#pragma unroll
-                                for (int b = 0; b < BLOCKS; ++b)
-                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + k * d + 16 * b) = gk[b] + gv[b];
-                            } else {
-#pragma unroll
-                                for (int b = 0; b < BLOCKS; ++b)
-                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + k * d + 16 * b) = gk[b];
-#pragma unroll
-                                for (int b = 0; b < BLOCKS; ++b)
-                                    if (FULL || 16 * b + 4 * g < d) *reinterpret_cast<f32x4*>(to + a.value_at + k * d + 16 * b) = gv[b];
-                            }
+                                for (int t = 0; t < N; ++t) {
+                                    y[b][t] = element(a.q, 0, b0 + b, t);
+                                    also[b][t] = element(f.grad_out, 0, b0 + b, t);
+                                }
+                            __builtin_amdgcn_sched_barrier(0);           // all on their way before the first is used
+                            of_part(y, also, false, b0);
+                            if (a.value_at) of_part(also, also, true, b0);
                         }
                     }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < X::NU; ++u)
+                        with_rows(u, [&](bool blank, auto zero, auto to_stage, auto to_rows, auto write_rows) {
+#pragma unroll
+                            for (int k = 0; k < PACK; ++k) {
+                                f32x4 gk[SOME], gv[SOME];
+                                zero(gk);
+                                zero(gv);
+                                of_head(qt[k], turn_ds, u, k, gk);
+                                of_head(gt[k], turn_p, u, k, gv);
+                                if (!all_seen && blank) {
+                                    zero(gk);
+                                    zero(gv);
+                                }
+                                if (a.value_at == 0) {
+#pragma unroll
+                                    for (int b = 0; b < SOME; ++b) gk[b] += gv[b];
+                                }
+                                if constexpr (L::STAGED) {
+                                    to_stage(gk, k * DP);
+                                    if (a.value_at) to_stage(gv, L::STRETCH + k * DP);
+                                } else if (FULL || k < heads) {
+                                    to_rows(gk, k * d, 0);
+                                    if (a.value_at) to_rows(gv, a.value_at + k * d, 0);
+                                }
+                            }
+                            if constexpr (L::STAGED) {
+                                if (a.value_at) write_rows(std::integral_constant<int, 2>(), 0);
+                                else write_rows(one, 0);
+                            }
+                        });
                 }
             };
             if (STEPS > 1 && group <= 4) row_gradients(std::integral_constant<int, 1>());
@@ -485,11 +632,9 @@ struct BwdPlan {
         pack = attn_pack(at, dp);
         chunks = (at->kv_heads + pack - 1) / pack;
         units = (uint32_t)((n >> kUnitShift) + bags);
-        waves = (uint32_t)std::min<int64_t>(units, most_waves(dp, pack, chunks));
-        groups = (waves + kBwdWaves - 1) / kBwdWaves;
+        waves = (uint32_t)std::min<int64_t>(units, std::max(1, 256 * kBwdWaves * bwd_groups_a_cu(elem_bytes(dtype), dp, dp * pack) / chunks));
+        groups = (waves + kBwdWaves - 1) / kBwdWaves;                    // what the chip holds at once
     }
-    // what the chip holds at once
-    static int64_t most_waves(int dp, int pack, int chunks) { return std::max<int64_t>(1, 1024 * (dp * pack > 64 ? 1 : 2) / chunks); }
 };
 
 struct BwdScratch {
@@ -503,6 +648,7 @@ struct BwdScratch {
     }
 };
 
+constexpr size_t kLdsMost = 160 << 10;            // of a workgroup
 struct BwdLaunch {
     const BwdArgs& f;
     const BwdPlan& l;
@@ -510,7 +656,10 @@ struct BwdLaunch {
     template <typename T, int DP, int PACK, bool FULL>
     int run() {
         const int cols = std::min(PACK, f.a.kv_heads) * (f.a.q_heads / f.a.kv_heads);
-        const size_t shared = BwdLds<T>::floats(f.a.bias ? f.a.rp.rows() : 0, cols) * 4;
+        const size_t shared = BwdLds<T, DP, PACK, FULL>::floats(f.a.bias ? f.a.rp.rows() : 0, cols) * 4;
+        if constexpr (FULL) {
+            if (shared > kLdsMost) return run<T, DP, PACK, false>();     // the largest tables leave no room for whole rows
+        }
         BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_kernel<T, DP, PACK, FULL>), dim3(l.groups, (unsigned)l.chunks), dim3(kBwdBlock), shared, stream, f);
         return BP_OK;
     }

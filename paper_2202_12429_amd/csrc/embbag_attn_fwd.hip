@@ -142,7 +142,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     typedef AttnTile<T, DP, PACK> X;
     typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
     const AttnArgs& a = f.a;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0), d = FULL ? DP : a.d;
     constexpr int stripes = kFwdWaves;
     const int stripe = wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * d;
@@ -183,12 +183,12 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
             float v[8];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float4 t = have ? *reinterpret_cast<const float4*>(q + at + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4 t = or_zeros(*reinterpret_cast<const float4*>(q + (FULL || at < d ? at : 0) + 4 * i), have);
                 v[4 * i] = t.x, v[4 * i + 1] = t.y, v[4 * i + 2] = t.z, v[4 * i + 3] = t.w;
             }
             qf[m].set(v);
         } else {
-            const float4 t = have ? *reinterpret_cast<const float4*>(q + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 t = or_zeros(*reinterpret_cast<const float4*>(q + (FULL || at < d ? at : 0)), have);
             qf[m] = f32x4{t.x, t.y, t.z, t.w};
         }
     }
@@ -290,13 +290,23 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
         for (int e = 0; e < X::PER; ++e) row_t[e] = tile[32 + X::PER * g + e];
         float most = -INFINITY;
+        if (a.cap > 0) {                          // (tests of what the call has stay outside the loops over entries)
 #pragma unroll
-        for (int e = 0; e < X::PER; ++e) {
-            float c = a.cap > 0 ? a.cap * tanh_few_ulp(z[e] * by_cap) : z[e] * a.scale;
-            if (a.bias) c += column[max(row_t[e], 0)];
-            z[e] = row_t[e] >= 0 ? c : -INFINITY;
-            most = fmaxf(most, z[e]);
+            for (int e = 0; e < X::PER; ++e) z[e] = a.cap * tanh_few_ulp(z[e] * by_cap);
+        } else {
+#pragma unroll
+            for (int e = 0; e < X::PER; ++e) z[e] *= a.scale;
         }
+        if (a.bias) {
+#pragma unroll
+            for (int e = 0; e < X::PER; ++e) z[e] += column[max(row_t[e], 0)];
+        }
+        if (!all_seen) {
+#pragma unroll
+            for (int e = 0; e < X::PER; ++e) z[e] = row_t[e] >= 0 ? z[e] : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < X::PER; ++e) most = fmaxf(most, z[e]);
         if (f.scores && col < cols) {
             const int e0 = t * X::ROWS + X::PER * g;
             float* const to = f.scores + head * f.score_stride + p.first + e0;
@@ -471,6 +481,7 @@ __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2
         if (x < wave) before += wave_sums[x];
         all += wave_sums[x];
     }
+    all = __builtin_amdgcn_readfirstlane(all);
     uint32_t at = even_start(blockIdx.x, all, f.groups);
     const uint32_t end = even_start(blockIdx.x + 1, all, f.groups);
 #pragma unroll
@@ -487,7 +498,7 @@ __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2
         }
     }
     __syncthreads();
-    uint32_t bag = start_bag, block = start_block;
+    uint32_t bag = __builtin_amdgcn_readfirstlane(start_bag), block = __builtin_amdgcn_readfirstlane(start_block);
     while (at < end && bag < bags) {
         const BagSpan s = bag_span(a, bag);
         const uint32_t mine = max(1u, (uint32_t)((s.count + kBlock - 1) >> kBlockShift)), take = min(mine - block, end - at);
