@@ -39,27 +39,22 @@ int attn_check_sizes(int64_t n, int64_t bags, size_t* bytes);
 struct BagSpan {
     int64_t first, count;
 };
-__device__ __forceinline__ BagSpan bag_span(const AttnArgs& a, int64_t bag) {
-    int64_t first = a.bag_off[bag], end = a.bag_off[bag + 1];
+__device__ __forceinline__ BagSpan bag_span(const AttnArgs& a, int64_t first, int64_t end, int64_t used) {
     if (first < 0) first = 0;
     if (end > a.n) end = a.n;
     int64_t count = end > first ? end - first : 0;
-    if (a.bag_len) {
-        const int64_t used = a.bag_len[bag];
-        if (used < count) count = used > 0 ? used : 0;
-    }
+    if (used < count) count = used > 0 ? used : 0;
     return {first, count};
 }
-
-__device__ __forceinline__ float row_value(const float* row, int64_t i) { return row[i]; }
-__device__ __forceinline__ float row_value(const uint16_t* row, int64_t i) { return bf16_bits_to_f32(row[i]); }
+__device__ __forceinline__ BagSpan bag_span(const AttnArgs& a, int64_t bag) {
+    return bag_span(a, a.bag_off[bag], a.bag_off[bag + 1], a.bag_len ? a.bag_len[bag] : a.n);
+}
 
 // Bags are handed out in pieces of 1 << shift entries, numbered without a scan over the bags: numbers below `bags` are the bags'
 // first pieces; the others of bag b begin at bags + (its offset >> shift), which leaves every bag room for all of its pieces (and
 // some numbers without one).
 inline int64_t piece_count(int64_t n, int64_t bags, int shift) { return (n >> shift) + bags; }
-__device__ __forceinline__ uint32_t more_pieces(const AttnArgs& a, int shift, uint32_t bag) {
-    int64_t at = a.bag_off[bag];
+__device__ __forceinline__ uint32_t more_pieces(const AttnArgs& a, int shift, int64_t at) {
     if (at < 0) at = 0;
     if (at > a.n) at = a.n;
     return (uint32_t)(at >> shift);
@@ -71,10 +66,9 @@ struct BagPiece {
     int64_t first;                    // its entries
     int count;
 };
-__device__ __forceinline__ uint32_t piece_id(const BagPiece& p, uint32_t number) { return number == 0 ? p.bag : p.more + number - 1; }
-__device__ __forceinline__ BagPiece bag_piece(const AttnArgs& a, int shift, uint32_t bag, uint32_t number, const BagSpan& s) {
+__device__ __forceinline__ BagPiece bag_piece(const AttnArgs& a, int shift, uint32_t bag, uint32_t number, const BagSpan& s, int64_t offset) {
     BagPiece p;
-    const uint32_t at = more_pieces(a, shift, bag), extra = (uint32_t)(a.n >> shift);
+    const uint32_t at = more_pieces(a, shift, offset), extra = (uint32_t)(a.n >> shift);
     p.bag = bag;
     p.number = number;
     p.more = (uint32_t)a.bags + at;
@@ -83,41 +77,17 @@ __device__ __forceinline__ BagPiece bag_piece(const AttnArgs& a, int shift, uint
     p.count = number < p.of ? (int)min(int64_t(1) << shift, s.count - ((int64_t)number << shift)) : 0;
     return p;
 }
-// A multiplier that spreads 0 .. count - 1 over themselves (count and it have no common factor).
-inline uint32_t spread_of(int64_t count) {
-    if (count < 3) return 1;
-    uint64_t k = (uint64_t)(0.6180339887 * (double)count) | 1;
-    const auto common = [](uint64_t a, uint64_t b) {
-        while (b) {
-            const uint64_t t = a % b;
-            a = b;
-            b = t;
-        }
-        return a;
-    };
-    while (common(k, (uint64_t)count) != 1) ++k;
-    return (uint32_t)(k % (uint64_t)count);
-}
-
-// Workgroup w's piece number.  Bags with room to grow have real pieces first and then numbers without one, at distances that tend
-// to be powers of two; taken in order, some of the chip's eight dies, to which workgroups are dealt in turn, get most of the real
-// ones (64 lists of up to 8,192 entries in stretches of 8,192: 117 us in order, 87 spread).
-__device__ __forceinline__ uint32_t spread_piece(const AttnArgs& a, int shift, uint32_t spread, uint32_t w) {
-    if (w < (uint32_t)a.bags) return w;
-    return (uint32_t)a.bags + (uint32_t)((uint64_t)(w - (uint32_t)a.bags) * spread % (uint64_t)(a.n >> shift));
-}
-
 // The piece with number `id`; behind the first pieces the bag is looked for, 64 bags a step by every wavefront.
 __device__ __forceinline__ BagPiece find_piece(const AttnArgs& a, int shift, uint32_t id) {
-    if (id < (uint32_t)a.bags) return bag_piece(a, shift, id, 0, bag_span(a, id));
+    if (id < (uint32_t)a.bags) return bag_piece(a, shift, id, 0, bag_span(a, id), a.bag_off[id]);
     const uint32_t lane = threadIdx.x % 64, x = id - (uint32_t)a.bags;
     uint32_t lo = 0, hi = (uint32_t)a.bags;
     while (hi - lo > 1) {             // the last bag whose numbers begin no later
         const uint32_t step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step;
-        lo += __popcll(__ballot(i < hi && more_pieces(a, shift, i) <= x)) * step;
+        lo += __popcll(__ballot(i < hi && more_pieces(a, shift, a.bag_off[i]) <= x)) * step;
         hi = min(hi, lo + step);
     }
-    return bag_piece(a, shift, lo, x - more_pieces(a, shift, lo) + 1, bag_span(a, lo));
+    return bag_piece(a, shift, lo, x - more_pieces(a, shift, a.bag_off[lo]) + 1, bag_span(a, lo), a.bag_off[lo]);
 }
 
 // exp of a difference: scores stay in natural units up to here, so that the lowest fp32 value, which masks give, does not become

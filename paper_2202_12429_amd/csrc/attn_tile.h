@@ -70,7 +70,7 @@ __device__ __forceinline__ uint2 masked(const uint2& v, uint32_t m) { return mak
 __device__ __forceinline__ uint32_t masked(uint32_t v, uint32_t m) { return v & m; }
 
 // head_dim rounded up, and the kv heads that share a wavefront's columns: as many as have columns, and registers for two
-// workgroups a CU (forward, four heads of 64, rows of 1 KB: 120 us with all four in one workgroup, one a CU, 99 with two).
+// workgroups a CU (forward, four heads of 64, rows of 1 KB: 67 us by twos, 70 one by one).
 inline int attn_dp(const bp_attn* at, int dtype) {
     int dp = dtype == BP_F32 ? 16 : 32;
     while (dp < at->head_dim) dp *= 2;
@@ -109,6 +109,59 @@ int dispatch_attn(const AttnArgs& a, int dp, int pack, F&& f) {
         case 256: return dispatch_attn_pack<T, 256>(a, pack, f);
     }
     return fail(BP_ERR_UNSUPPORTED, "no layout for heads of %d", dp);
+}
+
+// Rows without the matrix instructions: a lane holds 16 bytes, LANES lanes a head.
+template <typename T, int LANES>
+struct Narrow {
+    static constexpr int VE = 16 / sizeof(T), D = LANES * VE;
+    static __device__ __forceinline__ void read(const float* from, float (&v)[VE]) {
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) __builtin_memcpy(v + i, __builtin_assume_aligned(from + i, 16), 16);
+    }
+    static __device__ __forceinline__ void write(float* to, const float (&v)[VE]) {
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) __builtin_memcpy(__builtin_assume_aligned(to + i, 16), v + i, 16);
+    }
+    static __device__ __forceinline__ void widen(const uint4& x, float (&v)[VE]) {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (VE == 4) {
+                v[i] = __uint_as_float(w[i]);
+            } else {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
+    // the same sum in all of the head's lanes
+    static __device__ __forceinline__ float dot(const float (&x)[VE], const float (&y)[VE]) {
+        float s = x[0] * y[0];
+#pragma unroll
+        for (int i = 1; i < VE; ++i) s = fmaf(x[i], y[i], s);
+#pragma unroll
+        for (int off = 1; off < LANES; off <<= 1) s += __shfl_xor(s, off);
+        return s;
+    }
+};
+// One query head a kv head, rows that are their own values, and lanes that heads and rows divide evenly.
+inline bool attn_narrow(const bp_attn* at, int dtype) {
+    const int lanes = at->head_dim * (dtype == BP_F32 ? 4 : 2) / 16, width = lanes * at->kv_heads;
+    const auto power = [](int x) { return x > 0 && (x & (x - 1)) == 0; };
+    return at->q_heads == at->kv_heads && at->value_offset == 0 && at->head_dim >= 16 && power(at->head_dim) && power(at->kv_heads) && width <= 64;
+}
+template <typename T, typename F>
+int dispatch_narrow(const AttnArgs& a, F&& f) {
+    switch (a.d * (int)sizeof(T) / 16) {
+        case 2: if constexpr (sizeof(T) == 2) return f.template run_narrow<T, 2>(); break;
+        case 4: return f.template run_narrow<T, 4>();
+        case 8: return f.template run_narrow<T, 8>();
+        case 16: return f.template run_narrow<T, 16>();
+        case 32: return f.template run_narrow<T, 32>();
+        case 64: if constexpr (sizeof(T) == 4) return f.template run_narrow<T, 64>(); break;
+    }
+    return fail(BP_ERR_UNSUPPORTED, "no layout for heads of %d", a.d);
 }
 
 __device__ __forceinline__ float4 or_zeros(const float4& v, bool have) {

@@ -42,6 +42,44 @@ __device__ __forceinline__ uint32_t share_of(uint32_t unit, uint32_t units, uint
     return min((uint32_t)(((uint64_t)(unit + 1) * waves - 1) / units), waves - 1);
 }
 
+// A wavefront's bags, or parts of them: body(bag, first entry, entries, all that the bag uses?, its beginning?).
+template <typename F>
+__device__ __forceinline__ void for_own_bags(const BwdArgs& f, uint32_t share, F&& body) {
+    const AttnArgs& a = f.a;
+    const int lane = threadIdx.x % 64;
+    uint32_t at = share < f.waves ? share_start(share, f.units, f.waves) : f.units;
+    const uint32_t end = share < f.waves ? share_start(share + 1, f.units, f.waves) : f.units;
+    uint32_t bag = 0;
+    if (at < end) {
+        uint32_t hi = (uint32_t)a.bags;
+        while (hi - bag > 1) {                                           // the last bag that begins no later, 64 bags a step
+            const uint32_t step = (hi - bag + 63) / 64, i = bag + (lane + 1) * step;
+            bag += __popcll(__ballot(i < hi && first_unit(a, i) <= at)) * step;
+            hi = min(hi, bag + step);
+        }
+    }
+    for (; at < end && bag < (uint32_t)a.bags; ++bag) {
+        // the bag's units from `at` on that are this wavefront's
+        const BagSpan s = bag_span(a, bag);
+        const uint32_t from = first_unit(a, bag), mine = max(1u, (uint32_t)((s.count + kUnit - 1) >> kUnitShift));
+        const uint32_t begin = at - min(at, from), stop = min(mine, end - min(end, from));
+        const bool starts = begin == 0, whole = starts && stop == mine;
+        at = bag + 1 < (uint32_t)a.bags ? max(at, first_unit(a, bag + 1)) : end;
+        if (begin >= stop) continue;                                     // numbers without a unit
+        body(bag, s.first + ((int64_t)begin << kUnitShift), (int)min(s.count - ((int64_t)begin << kUnitShift), (int64_t)(stop - begin) << kUnitShift), whole, starts);
+    }
+}
+// Elements of the rows that are neither key nor value.
+__device__ __forceinline__ void clear_rest(const BwdArgs& f, int64_t first, int count) {
+    const AttnArgs& a = f.a;
+    const int span = a.kv_heads * a.d, behind = a.value_at + span, gap = a.value_at == 0 ? 0 : a.value_at - span;
+    if (gap + a.dim - behind > 0)
+        for (int64_t e = threadIdx.x % 64; e < (int64_t)count * (gap + a.dim - behind); e += 64) {
+            const int x = (int)(e % (gap + a.dim - behind));
+            f.grad_rows[(first + e / (gap + a.dim - behind)) * a.dim + (x < gap ? span + x : behind + x - gap)] = 0.f;
+        }
+}
+
 // LDS: borders, the bias table's columns of the workgroup's heads; of every wavefront two tiles' slots and table rows, a tile's ds and p
 // entry by entry, and four tables of sums, one for each quarter of the wavefront, in which a column is one lane's.
 // STAGE: 16 entries' row gradients, to be written out a row at a time: keys' and values', or, of wide heads, a stretch of either.
@@ -56,6 +94,8 @@ struct BwdLds {
 
 // Workgroups that a CU holds, by their registers.
 constexpr int bwd_groups_a_cu(size_t elem, int dp, int flat) { return flat <= 32 || (elem == 4 && dp <= 32 && flat <= 64) ? 2 : 1; }
+
+constexpr int kNarrowGroups = 4;         // of the kernel without matrix instructions
 
 template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK)) void embbag_attn_bwd_kernel(BwdArgs f) {
@@ -72,7 +112,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     const int d = FULL ? DP : a.d;
     const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0);
-    const int first_head = kv0 * group, cols = heads * group, flat = heads * d, span = a.kv_heads * d;
+    const int first_head = kv0 * group, cols = heads * group, flat = heads * d;
     const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;
     const int table_rows = a.bias ? a.rp.rows() : 0;
 
@@ -91,33 +131,12 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
     }
 
     const uint32_t share = blockIdx.x * kBwdWaves + wave;
-    uint32_t at = share < f.waves ? share_start(share, f.units, f.waves) : f.units;
-    const uint32_t end = share < f.waves ? share_start(share + 1, f.units, f.waves) : f.units;
-    uint32_t bag = 0;
-    if (at < end) {
-        uint32_t hi = (uint32_t)a.bags;
-        while (hi - bag > 1) {                                           // the last bag that begins no later, 64 bags a step
-            const uint32_t step = (hi - bag + 63) / 64, i = bag + (lane + 1) * step;
-            bag += __popcll(__ballot(i < hi && first_unit(a, i) <= at)) * step;
-            hi = min(hi, bag + step);
-        }
-    }
     const T* const w = (const T*)a.cache_w + (int64_t)kv0 * d;
     const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
     int sum_row = -1;                                                    // the lane's running sum for the bias table, and its row
     float sum_dz = 0.f;
 
-    for (; at < end && bag < (uint32_t)a.bags; ++bag) {
-        // the bag's units from `at` on that are this wavefront's
-        const BagSpan s = bag_span(a, bag);
-        const uint32_t from = first_unit(a, bag), mine = max(1u, (uint32_t)((s.count + kUnit - 1) >> kUnitShift));
-        const uint32_t begin = at - min(at, from), stop = min(mine, end - min(end, from));
-        const bool starts = begin == 0, whole = starts && stop == mine;
-        at = bag + 1 < (uint32_t)a.bags ? max(at, first_unit(a, bag + 1)) : end;
-        if (begin >= stop) continue;                                     // numbers without a unit
-        const int64_t first = s.first + ((int64_t)begin << kUnitShift);
-        const int count = (int)min(s.count - ((int64_t)begin << kUnitShift), (int64_t)(stop - begin) << kUnitShift);
-
+    for_own_bags(f, share, [&](uint32_t bag, int64_t first, int count, bool whole, bool starts) {
         // q and grad_out: for the products with rows, and (a column a quarter) for those with ds and p
         const float* const q = a.q + ((int64_t)bag * a.q_heads + head) * d;
         const float* const go = f.grad_out + ((int64_t)bag * a.q_heads + head) * d;
@@ -533,13 +552,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
                             dq[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kv[e][m], j)), ds[e], dq[m][j], 0, 0, 0);
             }
         }
-        // elements of the rows that are neither key nor value
-        const int behind = a.value_at + span, gap = a.value_at == 0 ? 0 : a.value_at - span;
-        if (blockIdx.y == 0 && gap + a.dim - behind > 0)
-            for (int64_t e = lane; e < (int64_t)count * (gap + a.dim - behind); e += 64) {
-                const int x = (int)(e % (gap + a.dim - behind));
-                f.grad_rows[(first + e / (gap + a.dim - behind)) * a.dim + (x < gap ? span + x : behind + x - gap)] = 0.f;
-            }
+        if (blockIdx.y == 0) clear_rest(f, first, count);
         float* const to = (whole ? f.grad_q + ((int64_t)bag * a.q_heads + head) * d
                                  : f.parts + ((2 * (int64_t)share + starts) * a.q_heads + head) * d) - own * d;
 #pragma unroll
@@ -552,7 +565,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
                 for (int j = 0; j < X::VW; ++j) v[j] = dq[m][j][i];
                 if (col < cols && x >= own * d && x < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + x, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
             }
-    }
+    });
     if (!a.bias) return;
     if (sum_row >= 0 && col < cols) sums[sum_row * 16] += sum_dz;
     __syncthreads();
@@ -561,6 +574,105 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
         double sum = 0;
         for (int x = 0; x < kBwdWaves * 4; ++x) sum += all[(x * table_rows + e / cols) * 16 + e % cols];
         f.bias_parts[((int64_t)blockIdx.x * table_rows + e / cols) * a.q_heads + first_head + e % cols] = (float)sum;
+    }
+}
+
+// One query head a kv head, and rows that are their own values, without the matrix instructions, as in the forward pass: a lane holds 16
+// bytes of a row and writes their gradients, rows side by side.  (8,192 bags of up to 50 rows, 4 heads of 16: 40 us in fp32 and 29 in
+// bf16, through the matrix instructions 63 and 108.)
+template <typename T, int LANES>
+__global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narrow_kernel(BwdArgs f) {
+    extern __shared__ float lds[];
+    constexpr int kSteps = 4;
+    typedef Narrow<T, LANES> N;
+    const AttnArgs& a = f.a;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int width = a.kv_heads * LANES, r = lane / width, head = lane % width / LANES, at = lane % LANES * N::VE;
+    const int side = 64 / width, d = N::D, heads = a.q_heads, table_rows = a.bias ? a.rp.rows() : 0;
+    int32_t* const borders = (int32_t*)lds;
+    float* const table = lds + 64;
+    float* const all_sums = table + table_rows * heads;                  // [wavefront][row side by side][table row][head]
+    float* const sums = all_sums + (wave * side + r) * table_rows * heads + head;
+    if (a.bias) {
+        if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = a.rp.borders[threadIdx.x];
+        for (int e = threadIdx.x; e < table_rows * heads; e += kBwdBlock) table[e] = a.bias[e];
+        for (int e = threadIdx.x; e < kBwdWaves * side * table_rows * heads; e += kBwdBlock) all_sums[e] = 0.f;
+        __syncthreads();
+    }
+    const T* const w = (const T*)a.cache_w + (int64_t)head * d + at;
+    const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
+    const uint32_t share = blockIdx.x * kBwdWaves + wave;
+    for_own_bags(f, share, [&](uint32_t bag, int64_t first, int count, bool whole, bool starts) {
+        const int64_t place = ((int64_t)bag * heads + head) * d + at;
+        float q[N::VE], go[N::VE], out[N::VE], dq[N::VE];
+        N::read(a.q + place, q);
+        N::read(f.grad_out + place, go);
+        N::read(f.out + place, out);
+        const float lse = f.lse[(int64_t)bag * heads + head], against = N::dot(go, out);
+        const int64_t q_pos = a.bias ? a.q_pos[bag] : 0;
+#pragma unroll
+        for (int i = 0; i < N::VE; ++i) dq[i] = 0.f;
+        int32_t slot_n = -1, pos_n = 0;
+        const auto fetch = [&](int e) {
+            slot_n = e + lane < count ? a.slots[first + e + lane] : -1;
+            pos_n = e + lane < count && a.bias ? a.lookup_pos[first + e + lane] : 0;
+        };
+        fetch(0);
+        for (int e0 = 0; e0 < count; e0 += 64) {
+            int row_of = -1;
+            if ((uint32_t)slot_n < (uint64_t)a.C) row_of = a.bias ? relpos_row(q_pos - pos_n, borders, a.rp.buckets, a.rp.two_sided) : 0;
+            const int slot = row_of >= 0 ? slot_n : 0, here = min(64, count - e0);
+            if (e0 + 64 < count) fetch(e0 + 64);
+            for (int s0 = 0; s0 < here; s0 += kSteps * side) {
+                uint4 raw[kSteps];
+                int row[kSteps];
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const int e = s0 + s * side + r;                     // (behind the 64th: an entry that is not there)
+                    row[s] = __shfl(row_of, e & 63);
+                    if (e >= here) row[s] = -1;
+                    const T* const from = w + (int64_t)__shfl(slot, e & 63) * a.wst;
+                    if (s0 + s * side < here) raw[s] = *reinterpret_cast<const uint4*>(from);
+                }
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    if (s0 + s * side >= here) break;
+                    float v[N::VE], grad[N::VE];
+                    N::widen(masked(raw[s], row[s] >= 0 ? ~0u : 0u), v);
+                    float z = N::dot(q, v), bend = a.scale;
+                    if (a.cap > 0) {
+                        const float t = tanh_few_ulp(z * by_cap);
+                        z = a.cap * t;
+                        bend = a.scale * fmaf(-t, t, 1.f);
+                    } else {
+                        z *= a.scale;
+                    }
+                    if (a.bias) z += table[max(row[s], 0) * heads + head];
+                    const float dp = N::dot(go, v);
+                    const bool in = row[s] >= 0 && z != -INFINITY;       // (these as in the kernel above)
+                    const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in && p != 1.f ? p * (dp - against) : 0.f, ds = dz * bend;
+                    if (a.bias && at == 0 && row[s] >= 0) sums[row[s] * heads] += dz;
+#pragma unroll
+                    for (int i = 0; i < N::VE; ++i) {
+                        grad[i] = row[s] >= 0 ? fmaf(ds, q[i], p * go[i]) : 0.f;
+                        dq[i] = fmaf(ds, v[i], dq[i]);
+                    }
+                    if (s0 + s * side + r < here) N::write(f.grad_rows + (first + e0 + s0 + s * side + r) * a.dim + head * d + at, grad);
+                }
+            }
+        }
+        clear_rest(f, first, count);
+        for (int off = width; off < 64; off <<= 1)
+#pragma unroll
+            for (int i = 0; i < N::VE; ++i) dq[i] += __shfl_xor(dq[i], off);
+        if (r == 0) N::write((whole ? f.grad_q + place : f.parts + ((2 * (int64_t)share + starts) * heads + head) * d + at), dq);
+    });
+    if (!a.bias) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < table_rows * heads; e += kBwdBlock) {
+        double sum = 0;
+        for (int x = 0; x < kBwdWaves * side; ++x) sum += all_sums[x * table_rows * heads + e];
+        f.bias_parts[(int64_t)blockIdx.x * table_rows * heads + e] = (float)sum;
     }
 }
 
@@ -609,17 +721,20 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_bwd_join_kernel(BwdArg
     }
 }
 
-// grad_bias from the workgroups' parts: 16 elements of the table a workgroup, 16 parts of them side by side
-__global__ __launch_bounds__(256) void embbag_attn_bias_join_kernel(const float* __restrict__ parts, int count, int groups, float* __restrict__ grad_bias) {
-    __shared__ double part[16][16];
+// grad_bias from the workgroups' parts: 16 elements of the table a workgroup, 64 parts of them side by side
+constexpr int kBiasJoinBlock = 1024;
+__global__ __launch_bounds__(kBiasJoinBlock) void embbag_attn_bias_join_kernel(const float* __restrict__ parts, int count, int groups, float* __restrict__ grad_bias) {
+    __shared__ double part[kBiasJoinBlock / 16][16];
     const int c = threadIdx.x % 16, e = blockIdx.x * 16 + c, share = threadIdx.x / 16;
     double sum = 0;
-    if (e < count)
-        for (int x = share; x < groups; x += 16) sum += parts[(int64_t)x * count + e];
+    if (e < count) {
+#pragma unroll 4
+        for (int x = share; x < groups; x += kBiasJoinBlock / 16) sum += parts[(int64_t)x * count + e];
+    }
     part[share][c] = sum;
     __syncthreads();
     if (share == 0 && e < count) {
-        for (int x = 1; x < 16; ++x) sum += part[x][c];
+        for (int x = 1; x < kBiasJoinBlock / 16; ++x) sum += part[x][c];
         grad_bias[e] = (float)sum;
     }
 }
@@ -627,12 +742,14 @@ __global__ __launch_bounds__(256) void embbag_attn_bias_join_kernel(const float*
 struct BwdPlan {
     int dp, pack, chunks;
     uint32_t units, waves, groups;
+    bool narrow;
     BwdPlan(const bp_attn* at, int dtype, int64_t n, int64_t bags) {
+        narrow = attn_narrow(at, dtype);
         dp = attn_dp(at, dtype);
         pack = attn_pack(at, dp);
-        chunks = (at->kv_heads + pack - 1) / pack;
+        chunks = narrow ? 1 : (at->kv_heads + pack - 1) / pack;
         units = (uint32_t)((n >> kUnitShift) + bags);
-        waves = (uint32_t)std::min<int64_t>(units, std::max(1, 256 * kBwdWaves * bwd_groups_a_cu(elem_bytes(dtype), dp, dp * pack) / chunks));
+        waves = (uint32_t)std::min<int64_t>(units, std::max(1, 256 * kBwdWaves * (narrow ? kNarrowGroups : bwd_groups_a_cu(elem_bytes(dtype), dp, dp * pack)) / chunks));
         groups = (waves + kBwdWaves - 1) / kBwdWaves;                    // what the chip holds at once
     }
 };
@@ -662,6 +779,16 @@ struct BwdLaunch {
         }
         BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_kernel<T, DP, PACK, FULL>), dim3(l.groups, (unsigned)l.chunks), dim3(kBwdBlock), shared, stream, f);
         return BP_OK;
+    }
+    template <typename T, int LANES>
+    int run_narrow() {
+        const size_t shared = (64 + (f.a.bias ? (size_t)f.a.rp.rows() * (f.a.q_heads + kBwdWaves * 64 / LANES) : 0)) * 4;
+        BP_LAUNCH(K_ATTN_BWD, (embbag_attn_bwd_narrow_kernel<T, LANES>), dim3(l.groups), dim3(kBwdBlock), shared, stream, f);
+        return BP_OK;
+    }
+    template <typename T>
+    int start() {
+        return l.narrow ? dispatch_narrow<T>(f.a, *this) : dispatch_attn<T>(f.a, l.dp, l.pack, *this);
     }
 };
 
@@ -709,7 +836,7 @@ BP_EXPORT int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const 
     f.bias_parts = w.bias_parts;
     if (bags) {
         BwdLaunch launch{f, l, stream};
-        BP_TRY(cfg->weight_dtype == BP_F32 ? dispatch_attn<float>(f.a, l.dp, l.pack, launch) : dispatch_attn<uint16_t>(f.a, l.dp, l.pack, launch));
+        BP_TRY(cfg->weight_dtype == BP_F32 ? launch.start<float>() : launch.start<uint16_t>());
         if (l.waves > 1) {
             const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
             const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);
@@ -718,7 +845,7 @@ BP_EXPORT int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const 
         }
     }
     if (rp)
-        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bias_join_kernel, dim3((unsigned)ceil_div(count, 16)), dim3(256), 0, stream, w.bias_parts, count,
+        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bias_join_kernel, dim3((unsigned)ceil_div(count, 16)), dim3(kBiasJoinBlock), 0, stream, w.bias_parts, count,
                   bags ? (int)l.groups : 0, grad_bias);
     return BP_OK;
 }

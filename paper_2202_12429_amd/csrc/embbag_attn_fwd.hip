@@ -87,7 +87,7 @@ namespace {
 struct FwdArgs {
     AttnArgs a;
     int32_t shift;              // log2 of a piece's entries
-    uint32_t pieces, spread;
+    uint32_t pieces;
     uint32_t groups;            // workgroups that share all entries evenly; 0: a workgroup a piece
     uint32_t* blocks;           // [bags + 1] running count of the bags' blocks, written by the first of these workgroups
     int32_t weighed;            // bags of one piece have their weights from the first launch
@@ -106,10 +106,10 @@ struct FwdArgs {
 template <int BLOCK>
 __device__ __forceinline__ void add_weights(const FwdArgs& f, uint32_t bag, int64_t first, int count) {
     const float* const lse = f.lse + (int64_t)bag * f.a.q_heads;
-    for (int i = threadIdx.x; i < count; i += BLOCK) {
+    for (int i = threadIdx.x % BLOCK; i < count; i += BLOCK) {
         const int64_t k = first + i;
         float add = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int h = 0; h < f.a.q_heads; ++h) {
             const float c = f.scores[h * f.score_stride + k];
             add += c == -INFINITY ? 0.f : exp_few_ulp(c - lse[h]);
@@ -134,9 +134,28 @@ struct Segment {
     bool whole;
 };
 
+// The borders, and the bias table's columns of the workgroup's heads.
+template <int WAVES>
+__device__ __forceinline__ void read_table(const AttnArgs& a, float* lds, int first_head, int cols) {
+    if (!a.bias) return;
+    float* const table = lds + AttnLds<WAVES>::FREE;
+    if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) ((int32_t*)lds)[AttnLds<WAVES>::BORDERS + threadIdx.x] = a.rp.borders[threadIdx.x];
+    if (cols == a.q_heads)
+        for (int e = threadIdx.x; e < a.rp.rows() * cols; e += WAVES * 64) table[e] = a.bias[e];
+    else
+        for (int e = threadIdx.x; e < a.rp.rows() * cols; e += WAVES * 64) table[e] = a.bias[(e / cols) * a.q_heads + first_head + e % cols];
+}
+
+// What the first tile of a wavefront's next segment begins with, on its way during the one before.
+struct Ahead {
+    int32_t slot, pos;
+    int64_t q_pos;
+};
+
+// One segment: the workgroup's wavefronts take its tiles in turn, or (ALONE) each has a segment of its own.
 constexpr int kFwdWaves = 4, kFwdBlock = kFwdWaves * 64;
-template <typename T, int DP, int PACK, bool FULL>
-__device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float* lds) {
+template <typename T, int DP, int PACK, bool FULL, bool ALONE>
+__device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float* lds, const Ahead& ahead = Ahead{}) {
     typedef AttnLds<kFwdWaves> L;
     constexpr int kLdsBorders = L::BORDERS, kLdsTile = L::TILE, kLdsMl = L::ML, kLdsFree = L::FREE;
     typedef AttnTile<T, DP, PACK> X;
@@ -144,8 +163,8 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     const AttnArgs& a = f.a;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK, heads = FULL ? PACK : min(PACK, a.kv_heads - kv0), d = FULL ? DP : a.d;
-    constexpr int stripes = kFwdWaves;
-    const int stripe = wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * d;
+    constexpr int stripes = ALONE ? 1 : kFwdWaves;
+    const int stripe = ALONE ? 0 : wave, first_head = kv0 * group, cols = heads * group, table_cols = cols, flat = heads * d;
     const int head = first_head + min(col, cols - 1), own = min(col, cols - 1) / group;        // the column's query head, its kv head
 
     int32_t* const borders = (int32_t*)lds + kLdsBorders;
@@ -161,16 +180,10 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
         slot_n = have ? a.slots[p.first + e] : -1;
         pos_n = have && a.bias ? a.lookup_pos[p.first + e] : 0;
     };
-    fetch(stripe);
-    const int64_t q_pos = a.bias ? a.q_pos[p.bag] : 0;
-    if (a.bias) {
-        if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = a.rp.borders[threadIdx.x];
-        if (table_cols == a.q_heads)
-            for (int e = threadIdx.x; e < a.rp.rows() * table_cols; e += kFwdBlock) table[e] = a.bias[e];
-        else
-            for (int e = threadIdx.x; e < a.rp.rows() * table_cols; e += kFwdBlock)
-                table[e] = a.bias[(e / table_cols) * a.q_heads + first_head + e % table_cols];
-    }
+    if (ALONE) slot_n = ahead.slot, pos_n = ahead.pos;
+    else fetch(stripe);
+    const int64_t q_pos = ALONE ? ahead.q_pos : a.bias ? a.q_pos[p.bag] : 0;
+    if (!ALONE) read_table<kFwdWaves>(a, lds, first_head, cols);
 
     // the queries: lane col has the column's
     const float* const q = a.q + ((int64_t)p.bag * a.q_heads + head) * d;
@@ -192,7 +205,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
             qf[m] = f32x4{t.x, t.y, t.z, t.w};
         }
     }
-    if (a.bias) __syncthreads();
+    if (!ALONE && a.bias) __syncthreads();
 
     f32x4 o[X::MB][X::VW];
 #pragma unroll
@@ -374,6 +387,33 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
 
+    float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * d : f.part_o + ((int64_t)p.part * a.q_heads + head) * d) - own * d;
+    const auto write_norm = [&](float best, float l) {
+        if (p.whole) {
+            f.lse[(int64_t)p.bag * a.q_heads + head] = l == 0.f ? -INFINITY : best + __builtin_amdgcn_logf(l) * kLn2;
+        } else {
+            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2] = best;
+            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2 + 1] = l;
+        }
+    };
+    const auto write = [&](int at, const float (&v)[X::VW]) {        // VW elements that lie side by side, if they are the column's head's
+        if (col < cols && at >= own * d && at < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+    };
+    if constexpr (ALONE) {
+        if (g == 0 && col < cols) write_norm(top, sum);
+        const float by = !p.whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int m = 0; m < X::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[X::VW];
+#pragma unroll
+                for (int j = 0; j < X::VW; ++j) v[j] = o[m][j][i] * by;
+                write((m * 16 + 4 * g + i) * X::VW, v);
+            }
+        return;
+    }
+
     // the wavefronts meet: every lane leaves its sums, and takes up a fourth of the lane's own place of all four
     float* const ml = lds + kLdsMl;
     float* const ox = lds + kLdsFree;
@@ -403,19 +443,9 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
         for (int x = 0; x < kFwdWaves; ++x) k[x] = l == 0.f ? 0.f : k[x] * by;
     }
-    if (wave == 0 && g == 0 && col < cols) {
-        if (p.whole) {
-            f.lse[(int64_t)p.bag * a.q_heads + head] = l == 0.f ? -INFINITY : best + __builtin_amdgcn_logf(l) * kLn2;
-        } else {
-            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2] = best;
-            f.part_ml[((int64_t)p.part * a.q_heads + head) * 2 + 1] = l;
-        }
-    }
-    // VW elements of the column's head that lie side by side
-    float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * d : f.part_o + ((int64_t)p.part * a.q_heads + head) * d) - own * d;
+    if (wave == 0 && g == 0 && col < cols) write_norm(best, l);
 #pragma unroll
     for (int m = 0; m < X::MB; ++m) {
-        const int at = (m * 16 + 4 * g + wave) * X::VW;
         float v[X::VW];
 #pragma unroll
         for (int j = 0; j < X::VW; ++j) {
@@ -423,7 +453,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 #pragma unroll
             for (int x = 0; x < kFwdWaves; ++x) v[j] = fmaf(k[x], ox[x * kWaveO + ((m * X::VW + j) * 4 + wave) * 64 + lane], v[j]);
         }
-        if (col < cols && at >= own * d && at < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
+        write((m * 16 + 4 * g + wave) * X::VW, v);
     }
     __syncthreads();                                                 // LDS is free again, the bag's lse there
 }
@@ -432,17 +462,162 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_fwd_kernel(FwdArgs f) {
     extern __shared__ float lds[];
-    const uint32_t id = spread_piece(f.a, f.shift, f.spread, blockIdx.x);
+    const uint32_t id = blockIdx.x;
     const BagPiece p = find_piece(f.a, f.shift, id);
     if (p.number >= p.of) return;
-    attend<T, DP, PACK, FULL>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
+    attend<T, DP, PACK, FULL, false>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
     if (f.scores && p.of == 1 && f.weighed) add_weights<kFwdBlock>(f, p.bag, p.first, p.count);       // all heads were this workgroup's
+}
+
+// Short bags: every wavefront takes whole pieces, so that none waits for the others of a workgroup (20,000 bags of up to 50 rows, 4 heads of
+// 16 through the matrix instructions: 88 us by workgroups, 58 so; of up to 200: 46 and 48), and has the next piece's entries on their way
+// meanwhile.  body(segment, ahead); `rows`: entries whose slots it wants ahead.
+template <bool AHEAD, typename F>                                         // AHEAD: where registers are not what is short
+__device__ __forceinline__ void for_own_pieces(const FwdArgs& f, int rows, F&& body) {
+    const AttnArgs& a = f.a;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t waves = gridDim.x * kFwdWaves;
+    uint32_t id = blockIdx.x * kFwdWaves + wave;
+    if (id >= f.pieces) return;
+    const auto begin = [&](const BagPiece& p) {
+        const bool have = lane < rows && lane < p.count;
+        return Ahead{have ? a.slots[p.first + lane] : -1, have && a.bias ? a.lookup_pos[p.first + lane] : 0, a.bias ? a.q_pos[p.bag] : 0};
+    };
+    BagPiece p = find_piece(a, f.shift, id);
+    Ahead ahead = begin(p);
+    for (;;) {
+        const bool more = waves < f.pieces - id;
+        BagPiece next{};
+        Ahead next_ahead{};
+        if (AHEAD && more) {
+            next = find_piece(a, f.shift, id + waves);
+            next_ahead = begin(next);
+        }
+        if (p.number < p.of) {
+            body(Segment{p.bag, id, p.first, p.count, p.of == 1}, ahead);
+            if (f.scores && p.of == 1 && f.weighed) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+                add_weights<64>(f, p.bag, p.first, p.count);
+            }
+        }
+        if (!more) break;
+        id += waves;
+        p = AHEAD ? next : find_piece(a, f.shift, id);
+        ahead = AHEAD ? next_ahead : begin(p);
+    }
+}
+
+template <typename T, int DP, int PACK, bool FULL>
+__global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_short_kernel(FwdArgs f) {
+    extern __shared__ float lds[];
+    const AttnArgs& a = f.a;
+    const int group = a.q_heads / a.kv_heads, kv0 = blockIdx.y * PACK;
+    read_table<kFwdWaves>(a, lds, kv0 * group, min(PACK, a.kv_heads - kv0) * group);
+    if (a.bias) __syncthreads();
+    for_own_pieces<true>(f, AttnTile<T, DP, PACK>::ROWS, [&](const Segment& p, const Ahead& ahead) { attend<T, DP, PACK, FULL, true>(f, p, lds, ahead); });
+}
+
+// One query head a kv head, and rows that are their own values: the matrix instructions would run 16 columns for one, and read a row
+// twice.  A lane holds 16 bytes of a row, LANES lanes a head, 64 / (heads * LANES) rows side by side; a score is a sum over a head's
+// lanes, and every lane pools its own elements, rows side by side each with their own maximum and sum up to the end.  Bound by the way
+// from a slot to its row, with as many wavefronts as their registers let a CU hold.  (20,000 bags of up to 50 rows, 4 heads of 16: 34 us in
+// fp32 and 27 in bf16, through the matrix instructions 58 and 65; keys and values apart, 2 heads of 64 in bf16: 75 and 70, with two query
+// heads a kv head 151 and 71.)
+template <typename T, int LANES>
+__global__ __launch_bounds__(kFwdBlock, sizeof(T) == 4 ? 6 : 5) void embbag_attn_narrow_kernel(FwdArgs f) {
+    extern __shared__ float lds[];
+    constexpr int kSteps = 2;
+    typedef Narrow<T, LANES> N;
+    const AttnArgs& a = f.a;
+    const int lane = threadIdx.x % 64, width = a.kv_heads * LANES, r = lane / width, head = lane % width / LANES, at = lane % LANES * N::VE;
+    const int side = 64 / width, d = N::D;
+    const int32_t* const borders = (const int32_t*)lds;
+    const float* const table = lds + AttnLds<kFwdWaves>::FREE;
+    const T* const w = (const T*)a.cache_w + (int64_t)head * d + at;
+    const float by_cap = a.cap > 0 ? a.scale / a.cap : 0.f;
+    read_table<kFwdWaves>(a, lds, 0, a.q_heads);
+    if (a.bias) __syncthreads();
+    for_own_pieces<false>(f, 64, [&](const Segment& p, const Ahead& ahead) {
+        float q[N::VE], o[N::VE], top = -INFINITY, sum = 0.f;
+        N::read(a.q + ((int64_t)p.bag * a.q_heads + head) * d + at, q);
+#pragma unroll
+        for (int i = 0; i < N::VE; ++i) o[i] = 0.f;
+        int32_t slot_n = ahead.slot, pos_n = ahead.pos;
+        for (int e0 = 0; e0 < p.count; e0 += 64) {
+            int row_of = -1;
+            if ((uint32_t)slot_n < (uint64_t)a.C) row_of = a.bias ? relpos_row(ahead.q_pos - pos_n, borders, a.rp.buckets, a.rp.two_sided) : 0;
+            const int slot = row_of >= 0 ? slot_n : 0, here = min(64, p.count - e0);
+            if (e0 + 64 < p.count) {
+                const bool have = e0 + 64 + lane < p.count;
+                slot_n = have ? a.slots[p.first + e0 + 64 + lane] : -1;
+                pos_n = have && a.bias ? a.lookup_pos[p.first + e0 + 64 + lane] : 0;
+            }
+            for (int s0 = 0; s0 < here; s0 += kSteps * side) {
+                uint4 raw[kSteps];
+                int row[kSteps];
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const int e = s0 + s * side + r;                         // (behind the 64th: an entry that is not there)
+                    row[s] = __shfl(row_of, e & 63);
+                    if (e >= here) row[s] = -1;
+                    const T* const from = w + (int64_t)__shfl(slot, e & 63) * a.wst;
+                    if (s0 + s * side < here) raw[s] = *reinterpret_cast<const uint4*>(from);
+                }
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    if (s0 + s * side >= here) break;
+                    float v[N::VE];
+                    N::widen(masked(raw[s], row[s] >= 0 ? ~0u : 0u), v);
+                    float z = N::dot(q, v);
+                    z = a.cap > 0 ? a.cap * tanh_few_ulp(z * by_cap) : z * a.scale;
+                    if (a.bias) z += table[max(row[s], 0) * a.q_heads + head];
+                    if (row[s] < 0) z = -INFINITY;
+                    if (f.scores && at == 0 && s0 + s * side + r < here) f.scores[head * f.score_stride + p.first + e0 + s0 + s * side + r] = z;
+                    if (__ballot(z > top + 7.f || (top == -INFINITY && z > top))) {
+                        const float next = fmaxf(top, z), shrink = exp_few_ulp(top - (next == -INFINITY ? 0.f : next));
+                        sum *= shrink;
+#pragma unroll
+                        for (int i = 0; i < N::VE; ++i) o[i] *= shrink;
+                        top = next;
+                    }
+                    const float pr = exp_few_ulp(z - (top == -INFINITY ? 0.f : top));
+                    sum += pr;
+#pragma unroll
+                    for (int i = 0; i < N::VE; ++i) o[i] = fmaf(pr, v[i], o[i]);
+                }
+            }
+        }
+        for (int off = width; off < 64; off <<= 1) {
+            const float other = __shfl_xor(top, off), next = fmaxf(top, other), from = next == -INFINITY ? 0.f : next;
+            const float ka = exp_few_ulp(top - from), kb = exp_few_ulp(other - from);
+            sum = fmaf(sum, ka, __shfl_xor(sum, off) * kb);
+#pragma unroll
+            for (int i = 0; i < N::VE; ++i) o[i] = fmaf(o[i], ka, __shfl_xor(o[i], off) * kb);
+            top = next;
+        }
+        if (r) return;
+        const int64_t to = (int64_t)(p.whole ? p.bag : p.part) * a.q_heads + head;
+        const float by = !p.whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < N::VE; ++i) o[i] *= by;
+        N::write((p.whole ? f.out : f.part_o) + to * d + at, o);
+        if (at == 0) {
+            if (p.whole) {
+                f.lse[to] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+            } else {
+                f.part_ml[to * 2] = top;
+                f.part_ml[to * 2 + 1] = sum;
+            }
+        }
+    });
 }
 
 // Few long bags: as many workgroups as the chip holds share all entries evenly, in blocks of kBlock, wherever bags begin and end;
 // a part's fixed cost (the way to its first rows, the meeting of its wavefronts: 8 us in a busy memory) is then paid once and at
-// the same time everywhere, and no CU is left with a part more than another.  (64 bags of 4,096 entries, 1 KB rows: 512 workgroups
-// in order 65 us; bags of up to 8,192: 99 by pieces.)  Bag b's blocks have the numbers [blocks[b], blocks[b + 1]), an empty bag's
+// the same time everywhere, and no CU is left with a part more than another.  (Rows of 1 KB, 64 bags
+// of up to 8,192 entries: 67 us, by pieces 99; all of 4,096: 67 and 71; 1,024 bags of up to 700: 92 and 98.)  Bag b's blocks have the numbers [blocks[b], blocks[b + 1]), an empty bag's
 // one block among them; workgroup w takes those from w * all / groups on.
 constexpr int kBlockShift = 7, kBlock = 1 << kBlockShift, kEvenBags = 2048;
 __device__ __forceinline__ uint32_t bag_blocks(const AttnArgs& a, uint32_t bag) {
@@ -503,21 +678,23 @@ __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2
         const BagSpan s = bag_span(a, bag);
         const uint32_t mine = max(1u, (uint32_t)((s.count + kBlock - 1) >> kBlockShift)), take = min(mine - block, end - at);
         const int64_t skip = (int64_t)block << kBlockShift;
-        attend<T, DP, PACK, FULL>(f, Segment{bag, 2 * blockIdx.x + (block == 0), s.first + skip, (int)min(s.count - skip, (int64_t)take << kBlockShift), take == mine}, lds);
+        attend<T, DP, PACK, FULL, false>(f, Segment{bag, 2 * blockIdx.x + (block == 0), s.first + skip, (int)min(s.count - skip, (int64_t)take << kBlockShift), take == mine}, lds);
         at += take;
         block = 0;
         ++bag;
     }
 }
 
-// The parts of a bag of several: a workgroup sums 16 elements of their pooled rows, four a thread and 64 parts side by side, each
-// with the maximum and sum of its head, online as within a part.  Workgroups look through `each` bags for such bags.
-constexpr int kJoinBlock = 256, kShare = 16;
+// The parts of a bag of several: a workgroup sums 64 elements of their pooled rows, four a thread and 16 parts side by side, each
+// with the maximum and sum of its head, online as within a part.  Workgroups look through `each` bags for such bags.  (64 bags of 12
+// parts, 16 heads of 64: 4.8 us, by 16 elements and 64 parts side by side 10.3; two bags of 384: 5.2 and 4.4.)
+constexpr int kJoinBlock = 256, kShare = 64;
 __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f, int each) {
-    __shared__ float part[kJoinBlock / 64][4][6];
+    constexpr int ACROSS = kShare / 4;
+    __shared__ float part[kJoinBlock / 64][ACROSS][6];
     const AttnArgs& a = f.a;
     const int hq = a.q_heads, width = hq * a.d, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int at = blockIdx.y * kShare + threadIdx.x % 4 * 4, h = min(at / a.d, hq - 1);
+    const int at = blockIdx.y * kShare + threadIdx.x % ACROSS * 4, h = min(at / a.d, hq - 1);
     const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
     // the parts of a bag, and the number of its i-th
     const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
@@ -526,7 +703,7 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
             *first = min(even_owner(f.blocks[bag], all, f.groups), f.groups - 1);
             return min(even_owner(f.blocks[bag + 1] - 1, all, f.groups), f.groups - 1) - *first + 1;
         }
-        const BagPiece p = bag_piece(a, f.shift, bag, 0, bag_span(a, bag));
+        const BagPiece p = bag_piece(a, f.shift, bag, 0, bag_span(a, bag), a.bag_off[bag]);
         *first = p.more;
         return p.of;
     };
@@ -552,12 +729,12 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
             top = next;
         };
         constexpr int AHEAD = 4;
-        for (uint32_t i0 = threadIdx.x / 4; i0 < of; i0 += kJoinBlock / 4 * AHEAD) {
+        for (uint32_t i0 = threadIdx.x / ACROSS; i0 < of; i0 += kJoinBlock / ACROSS * AHEAD) {
             float2 ml[AHEAD];
             float4 v[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                const uint32_t i = i0 + j * (kJoinBlock / 4);
+                const uint32_t i = i0 + j * (kJoinBlock / ACROSS);
                 const bool have = i < of && at < width;
                 const int64_t id = part_id(i);
                 ml[j] = have ? *reinterpret_cast<const float2*>(f.part_ml + (id * hq + h) * 2) : make_float2(-INFINITY, 0.f);
@@ -567,14 +744,14 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
             for (int j = 0; j < AHEAD; ++j) take(ml[j].x, ml[j].y, v[j]);
         }
 #pragma unroll
-        for (int off = 4; off < 64; off <<= 1)
+        for (int off = ACROSS; off < 64; off <<= 1)
             take(__shfl_xor(top, off), __shfl_xor(l, off), make_float4(__shfl_xor(o.x, off), __shfl_xor(o.y, off), __shfl_xor(o.z, off), __shfl_xor(o.w, off)));
-        if (lane < 4) {
+        if (lane < ACROSS) {
             float* const x = part[wave][lane];
             x[0] = top, x[1] = l, x[2] = o.x, x[3] = o.y, x[4] = o.z, x[5] = o.w;
         }
         __syncthreads();
-        if (threadIdx.x < 4 && at < width) {
+        if (threadIdx.x < ACROSS && at < width) {
             for (int w = 1; w < kJoinBlock / 64; ++w) {
                 const float* const x = part[w][lane];
                 take(x[0], x[1], make_float4(x[2], x[3], x[4], x[5]));
@@ -593,23 +770,31 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
 constexpr int kWeightShift = 8;
 __global__ __launch_bounds__(kJoinBlock) void embbag_attn_weight_kernel(FwdArgs f) {
     const BagPiece p = find_piece(f.a, kWeightShift, blockIdx.x);
-    if (p.number >= p.of || (f.weighed && bag_piece(f.a, f.shift, p.bag, 0, bag_span(f.a, p.bag)).of == 1)) return;
+    if (p.number >= p.of || (f.weighed && bag_piece(f.a, f.shift, p.bag, 0, bag_span(f.a, p.bag), f.a.bag_off[p.bag]).of == 1)) return;
     add_weights<kJoinBlock>(f, p.bag, p.first, p.count);
 }
 
 // How a call is laid out.
-constexpr int kPieceShift = 9, kLongMean = 1 << kPieceShift;
+constexpr int kPieceShift = 9, kLongMean = 1 << kPieceShift, kShortMean = 64, kNarrowMean = 128, kManyBags = 2560;
 struct FwdPlan {
     int dp, pack, chunks;      // head_dim rounded up; kv heads a workgroup takes, and how many such shares there are
+    bool alone;                // a wavefront a piece
+    bool narrow;               // heads without the matrix instructions
     bool even;                 // bags of 512 entries and more in the mean, and not so many that each workgroup could not count them
-    uint32_t groups;           // what the chip holds at once
+    uint32_t resident, groups; // workgroups that the chip holds at once; and no more than have a block of entries
     FwdPlan(const bp_attn* at, int dtype, int64_t n, int64_t bags) {
         dp = attn_dp(at, dtype);
         pack = attn_pack(at, dp);
         chunks = (at->kv_heads + pack - 1) / pack;
         even = bags <= kEvenBags && n >= kLongMean * std::max<int64_t>(bags, 1);
         const int flat = pack * dp;
-        groups = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(256 * (flat > 128 ? 1 : flat > 64 ? 2 : 3) / chunks, (n >> kBlockShift) + bags));
+        resident = std::max(1, 256 * (flat > 128 ? 1 : flat > 64 ? 2 : 3) / chunks);
+        narrow = attn_narrow(at, dtype);
+        // More bags than workgroups at once, and short ones.  Without the matrix instructions also longer ones, if there are enough for half of
+        // the chip's wavefronts (heads of 16 fp32, bags of 250 entries in the mean: 8,000 141 us by workgroups and 126, 2,000 45 and 73).
+        alone = bags > resident && n < (!narrow ? kShortMean : bags > kManyBags ? kLongMean : kNarrowMean) * bags;
+        if (narrow && alone) chunks = 1;
+        groups = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(resident, (n >> kBlockShift) + bags));
     }
     // parts that a workspace for n has room for, whatever smaller call it serves
     static int64_t parts(int64_t n, int64_t bags) { return std::max((n >> kPieceShift) + bags, 2 * std::min<int64_t>(768, (n >> kBlockShift) + std::min<int64_t>(bags, kEvenBags))); }
@@ -643,8 +828,18 @@ struct FwdLaunch {
         const size_t shared = AttnLds<kFwdWaves>::bytes(DP * PACK, table);
         if (l.even)
             BP_LAUNCH(K_ATTN_FWD, (embbag_attn_even_kernel<T, DP, PACK, FULL>), dim3(f.groups, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+        else if (l.narrow && l.alone)
+            return dispatch_narrow<T>(f.a, *this);
+        else if (l.alone)
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_short_kernel<T, DP, PACK, FULL>), dim3(std::min(l.resident, (unsigned)ceil_div(f.pieces, kFwdWaves)), (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
         else
             BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK, FULL>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+        return BP_OK;
+    }
+    template <typename T, int LANES>
+    int run_narrow() {
+        const size_t shared = AttnLds<kFwdWaves>::FREE * 4 + (f.a.bias ? (size_t)f.a.rp.rows() * f.a.q_heads * 4 : 0);
+        BP_LAUNCH(K_ATTN_FWD, (embbag_attn_narrow_kernel<T, LANES>), dim3(std::min(4096u, (unsigned)ceil_div(f.pieces, kFwdWaves))), dim3(kFwdBlock), shared, stream, f);
         return BP_OK;
     }
 };
@@ -685,7 +880,6 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     f.groups = l.even ? l.groups : 0;
     f.blocks = w.blocks;
     f.scores = weights ? w.scores : nullptr;
-    f.spread = spread_of(n_lookups >> f.shift);
     f.score_stride = score_stride(n_lookups);
     f.weighed = l.chunks == 1 && !l.even;
     f.part_ml = w.part_ml;

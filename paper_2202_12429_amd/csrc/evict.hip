@@ -61,7 +61,8 @@ constexpr int kDigits = 3, kBins = 2048, kStretches = 16;
 constexpr int kPieceShift = 15, kPiece = 1 << kPieceShift;        // what 1,024 threads hold
 constexpr int kShift[kDigits] = {21, 10, 0}, kWidth[kDigits] = {11, 11, 10};
 
-constexpr int kFew = 8;           // up to so many leave: found one by one, which takes a barrier each instead of the digits' nine
+constexpr int kFew = 8;           // up to so many leave: found one by one, a barrier each (of 1,025 entries one: 8.7 us, four 11.0, eight
+                                  // 14.1, sixteen 20.1), instead of the digits' nine (14.1 to 14.6)
 
 struct Choice {
     uint32_t key;             // the largest key that leaves
@@ -466,7 +467,9 @@ __global__ __launch_bounds__(1024) void evict_scan_kernel(EvictArgs a) {
 
 constexpr int64_t kManyLists = 4096;
 // Lists of up to 2,048 entries in the mean: 256 threads a list, one launch.  Longer ones: 1,024 threads choose, and a second launch
-// moves, 16 wavefronts a list wherever there is room.  From 16,384 on (a workgroup holds twice that) by pieces.
+// moves, 16 wavefronts a list wherever there is room (lists of 4,000: 512 of them 23 us in one launch and 30 in two, 32 of them 11.3 and
+// 10.2; of 64 of 16,000 the longest would hold a CU up while others have none).  From 16,384 on (a workgroup holds twice that) by pieces
+// (64 of 22,000: 31 us, whole 42; 8 of 31,000: 32 and 43).
 bool lists_short(int64_t n, int64_t bags) { return n <= 2048 * std::max<int64_t>(bags, 1); }
 bool lists_long(int64_t n, int64_t bags) { return n > (kPiece / 2) * std::max<int64_t>(bags, 1) && n > kPiece; }
 

@@ -59,7 +59,8 @@ constexpr int64_t kBiasMost = int64_t(1) << 40;
 // A workgroup writes a stretch of keys for up to kBiasRows queries of one head.  What it writes depends on j - i alone, so the
 // looked-up values lie in LDS as one line, of which every query takes a stretch, shifted by one from the query before.  16
 // bytes a store, aligned in memory (the first and last of a row's chunks may be cut), whatever a row's own alignment.  bf16 lines
-// are kept as pairs, once from every even and once from every odd element on.  Bound by the stores.
+// are kept as pairs, once from every even and once from every odd element on.  Bound by the stores (15 heads,
+// 2,048 queries, 1,999 keys, bf16: 36 us, with non-temporal stores 40).
 constexpr int kBiasBlock = 256, kBiasRows = 32, kBiasChunks = 256;
 template <typename T>
 __global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, const float* __restrict__ table, int heads, int64_t lq,
@@ -194,11 +195,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void relpos_bias_bwd_kernel(GradAr
     constexpr int NB = B::NB;
     __shared__ double diag[kGradWaves][B::DIAGONALS], eights[kGradWaves][B::DIAGONALS / 8], more[kGradWaves][B::DIAGONALS / 64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    // Segments of a head differ in work (the corners of the grid, a one-sided bias's later keys), and a CU gets workgroups at a
-    // stride that often is a multiple of a head's: every head begins at another of them.
-    const uint32_t turn = (uint32_t)(((uint64_t)(blockIdx.y + blockIdx.z * gridDim.y) * 2654435769u >> 7) % gridDim.x);
-    const uint32_t group = blockIdx.x + turn < gridDim.x ? blockIdx.x + turn : blockIdx.x + turn - gridDim.x;
-    const int64_t job = (int64_t)group * kGradWaves + wave, jobs = (int64_t)a.bands * a.segments;
+    const int64_t job = (int64_t)blockIdx.x * kGradWaves + wave, jobs = (int64_t)a.bands * a.segments;
     const bool have = job < jobs;
     const int64_t band0 = a.first_band + job / a.segments * 64, seg0 = job % a.segments * a.steps;
     const int64_t kd = band0 + lane;                                   // the lane's block diagonal
@@ -356,7 +353,8 @@ int check_grid(int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t row
 }
 
 // Bands and segments of the walk.  Segments of 128 queries where those make 4,096 wavefronts or more, shorter ones in smaller
-// launches.
+// launches (3 x 5 grids of 777 x 1,001 fp32, enough being 1,024: 21.6 us; 4,096: 13.6;
+// 16,384: 13.2, but 2 x 16 grids of 2,048 x 2,048 bf16 then take 37.4 for 36.5).
 constexpr int kGradEnough = 4096;
 int grad_plan(const Relpos& r, int32_t dtype, int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t q_start, GradArgs* a) {
     const int block = 16 / (int)elem_bytes(dtype), shift = dtype == BP_F32 ? 2 : 3;
@@ -413,11 +411,8 @@ BP_EXPORT int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_
     if (heads == 0 || lq == 0 || lk == 0) return BP_OK;
     if (!table || !out) return fail(BP_ERR_INVALID_ARG, "NULL pointer");
     if (((uintptr_t)table & 3) || (uintptr_t)out % elem_bytes(out_dtype)) return fail(BP_ERR_INVALID_ARG, "table or out is not aligned to its element");
-    // a workgroup's keys: a chunk a thread; fewer where there are too few workgroups for the chip
-    const int per = 16 / (int)elem_bytes(out_dtype);
+    const int per = 16 / (int)elem_bytes(out_dtype), chunks = kBiasChunks;         // a workgroup's keys
     const int64_t row_blocks = ceil_div(lq, kBiasRows), all_chunks = ceil_div(lk, per);
-    int chunks = kBiasChunks;
-    while (chunks > 32 && heads * row_blocks * ceil_div(all_chunks, chunks) < 512) chunks /= 2;
     const int64_t tiles = ceil_div(all_chunks, chunks);
     if (tiles * row_blocks >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
     const dim3 grid((unsigned)(tiles * row_blocks), (unsigned)heads);

@@ -257,6 +257,24 @@ def test_attention_with_bias_and_room(dtype, hq, hk, d, shared, two_sided, cap, 
     Batch(dtype, hq, hk, d, shared, LENGTHS[lengths], cap=cap, bias=(LOG, two_sided), room=True).check()
 
 
+MANY = [int(x) for x in np.random.default_rng(12).integers(0, 9, 1100)]
+MANY[3], MANY[700], MANY[1099] = 1300, 65, 140
+
+
+@pytest.mark.parametrize("extra", [dict(), dict(cap=4.0, bias=(LOG, True), room=True)])
+@pytest.mark.parametrize("dtype,hq,hk,d,shared", [
+    ("f32", 4, 4, 16, True), ("f32", 4, 2, 16, False), ("f32", 2, 2, 32, False), ("f32", 8, 4, 64, True), ("f32", 1, 1, 128, False), ("f32", 2, 1, 256, True),
+    ("bf16", 8, 4, 16, False), ("bf16", 2, 2, 32, True), ("bf16", 8, 4, 64, False), ("bf16", 2, 1, 128, True), ("bf16", 1, 1, 256, False),
+    ("f32", 12, 4, 16, False), ("bf16", 3, 3, 64, False), ("bf16", 8, 2, 64, False), ("f32", 2, 1, 8, False), ("bf16", 10, 2, 40, True)])
+def test_attention_of_many_short_bags(dtype, hq, hk, d, shared, extra):
+    Batch(dtype, hq, hk, d, shared, MANY, **extra).check()
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d,shared", [("f32", 4, 2, 16, False), ("bf16", 8, 2, 32, False), ("bf16", 3, 3, 24, False)])
+def test_attention_over_rows_with_gaps_and_strides_in_short_bags(dtype, hq, hk, d, shared):
+    Batch(dtype, hq, hk, d, shared, MANY, gap=16, stride=48, bias=(LOG, True), far=True).check()
+
+
 @pytest.mark.parametrize("dtype,hq,hk,d,shared", [("f32", 4, 2, 16, False), ("bf16", 8, 2, 32, False), ("bf16", 3, 3, 24, False)])
 def test_attention_over_rows_with_gaps_and_strides(dtype, hq, hk, d, shared):
     Batch(dtype, hq, hk, d, shared, LENGTHS["edges"], gap=16, stride=48, bias=(LOG, True), far=True).check()
