@@ -511,6 +511,7 @@ int bp_relpos_update(const bp_config* cfg, const bp_relpos* rp, int32_t heads, f
  *     p = softmax of c over the bag's entries that are seen;  out[b,h] = sum p * value;  lse[b,h] = log sum exp(c)
  * An entry is seen when its slot lies in [0, capacity) and rp, if given, sees its distance.  A bag that sees nothing has
  * out = 0 and lse = -infinity; an entry that is not seen has no part in anything, whatever its row holds.
+ * NaN among what is seen goes through to what it has a part in; an infinity there may come out as NaN.
  * With lists of one sequence's cached tokens as bags this is the attention of one new token per sequence over its cache.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct bp_attn {

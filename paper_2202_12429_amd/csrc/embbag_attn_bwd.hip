@@ -104,7 +104,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
     typedef typename Bytes<X::VW * sizeof(T)>::type VRaw;
     constexpr int STEPS = PACK == 1 ? 4 : PACK == 2 ? 2 : 1;             // of four columns, in a head's group
     constexpr int BLOCKS = DP / 16, SOME = BLOCKS < 8 ? BLOCKS : 8;      // of 16 elements of a head; blocks whose gradients are in work at a time
-    // q and grad_out in registers all along a bag, where they fit; else from the caches, tile by tile (400,000 rows of 2 x 256 bf16: 430 us so,
+    // q and grad_out in registers all along a bag, where they fit; else from the caches, tile by tile (400,000 rows of 2 x 256 bf16: 460 us so,
     // 1370 with registers spilled)
     constexpr bool KEEP = DP <= 128;
     extern __shared__ float lds[];
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
                 for (int e = 0; e < X::PER; ++e) {
                     const float t = tanh_few_ulp(c[e] * by_cap);
                     z[e] = a.cap * t;
-                    bend[e] = a.scale * fmaf(-t, t, 1.f);
+                    bend[e] = a.scale * fmaxf(fmaf(-t, t, 1.f), 0.f);    // (0 for a NaN, which a row that nobody sees may give; one that is seen has p NaN)
                 }
             } else {
 #pragma unroll
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narr
                     if (a.cap > 0) {
                         const float t = tanh_few_ulp(z * by_cap);
                         z = a.cap * t;
-                        bend = a.scale * fmaf(-t, t, 1.f);
+                        bend = a.scale * fmaxf(fmaf(-t, t, 1.f), 0.f);
                     } else {
                         z *= a.scale;
                     }

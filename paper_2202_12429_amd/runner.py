@@ -270,6 +270,13 @@ class CachedEmbeddingTrainer:
                                    bags, grad_out, self._bwd_ws, self._tickets, stream=stream)
 
     # ---- (6) bags pooled by attention
+    # What these calls allocate belongs to the stream they run on.  Their workspace is the trainer's, as the backward pass's is: one stream at
+    # a time, and a call that is captured into a graph takes its own through the library's functions.
+    @staticmethod
+    def _on(stream):
+        import torch
+        return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) and stream else stream or None)
+
     def _attn_workspace(self, need: int):
         if self._attn_ws is None or self._attn_ws.numel() < need:
             import torch
@@ -283,9 +290,10 @@ class CachedEmbeddingTrainer:
         n = self.iter_offsets.item(i + 1) - self.iter_offsets.item(i)
         if self.plan_.lookup_slots is None:
             raise ValueError("attention over bags needs a slot per lookup; plan with slot_map=True")
-        out = torch.empty_like(q) if out is None else out
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if lse is None else lse
-        ws = self._attn_workspace(B.bp_embbag_attn_fwd_workspace_bytes(self.cfg, at, n, bags, given.get("weight_out") is not None))
+        with self._on(stream):
+            out = torch.empty_like(q) if out is None else out
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if lse is None else lse
+            ws = self._attn_workspace(B.bp_embbag_attn_fwd_workspace_bytes(self.cfg, at, n, bags, given.get("weight_out") is not None))
         B.bp_embbag_attn_fwd(self.cfg, at, self._cw, self.slots(i), bag_offsets_dev, bags, q, out, lse, ws, stream=stream, **given)
         return out, lse
 
@@ -295,15 +303,15 @@ class CachedEmbeddingTrainer:
         steps the rows.  Returns the gradients of q and, with relpos, of the bias table (bp_relpos_update steps that)."""
         import torch
         n, rp = self.iter_offsets.item(i + 1) - self.iter_offsets.item(i), given.get("relpos")
-        grad_q = torch.empty_like(q) if grad_q is None else grad_q
-        if rp is not None and grad_bias is None:
-            grad_bias = torch.empty_like(given["bias_table"])
-        if self._grad_rows is None or self._grad_rows.shape[0] < n:
-            self._grad_rows = torch.zeros((n, int(self.cfg.dim)), dtype=torch.float32, device=self.device)
-        elif given.get("bag_lengths") is not None:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) and stream else stream):
+        with self._on(stream):
+            grad_q = torch.empty_like(q) if grad_q is None else grad_q
+            if rp is not None and grad_bias is None:
+                grad_bias = torch.empty_like(given["bias_table"])
+            if self._grad_rows is None or self._grad_rows.shape[0] < n:
+                self._grad_rows = torch.empty((n, int(self.cfg.dim)), dtype=torch.float32, device=self.device)
+            if given.get("bag_lengths") is not None:
                 self._grad_rows[:n].zero_()                  # lookups that no bag uses have no gradient
-        ws = self._attn_workspace(B.bp_embbag_attn_bwd_workspace_bytes(self.cfg, at, rp, n, bags))
+            ws = self._attn_workspace(B.bp_embbag_attn_bwd_workspace_bytes(self.cfg, at, rp, n, bags))
         B.bp_embbag_attn_bwd(self.cfg, at, self._cw, self.slots(i), bag_offsets_dev, bags, q, out, lse, grad_out, grad_q,
                              self._grad_rows[:n], grad_bias, ws, stream=stream, **given)
         self.backward_update(i, None, n, self._grad_rows[:n], stream=stream, grouped=grouped)

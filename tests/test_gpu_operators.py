@@ -314,6 +314,22 @@ def test_attention_reads_nothing_outside_the_lookups(offsets):
     within(lse, l, t_l, "lse")
 
 
+@pytest.mark.parametrize("lengths", [[40, 0, 3, 700, 33], MANY])
+@pytest.mark.parametrize("dtype,hq,hk,d,shared", [("bf16", 8, 2, 32, False), ("f32", 6, 2, 24, True), ("f32", 4, 4, 16, True), ("bf16", 1, 1, 256, False),
+                                                  ("bf16", 2, 2, 64, True)])
+def test_attention_whatever_rows_that_nobody_sees_hold(dtype, hq, hk, d, shared, lengths):
+    """Row 0 of the cache and the row of the slots that a bias masks: the same bits for zeros and for NaN."""
+    b = Batch(dtype, hq, hk, d, shared, lengths, cap=4.0, bias=(LOG, False), room=True)
+    b.slots[b.slots == 0] = 1
+    got = []
+    for fill in (0.0, float("nan")):
+        b.cache[0], b.cache[-1] = fill, fill
+        out, lse, w = b.forward()
+        got.append((out, lse, w) + b.backward(out, lse))
+    for x, y in zip(*got):
+        assert not x.isnan().any() and torch.equal(x, y)
+
+
 def test_attention_lets_infinities_and_nan_through_where_they_are_seen():
     b = Batch("f32", 2, 1, 16, False, [4, 4, 4])
     c = torch.randn(997, 32, device=DEV)
@@ -631,3 +647,41 @@ def test_training_on_bags_pooled_by_attention(optimizer, dtype, grouping):
     got = W.double().cpu().numpy()
     assert np.abs(got - w).max() <= (1e-4 if dtype == "f32" else 0.05) * np.abs(w).max()
     assert np.abs(tab.double().cpu().numpy() - tab64).max() <= (1e-4 if dtype == "f32" else 0.05)
+
+
+@pytest.mark.parametrize("handle", [True, False])
+def test_training_on_bags_on_another_stream(handle):
+    """attend() and attend_backward_update() with lists that use part of their stretch, on a stream of the caller's: the same bits as
+    on the current one, and no gradient from lookups that no bag uses."""
+    from paper_2202_12429_amd.runner import CachedEmbeddingTrainer
+    rng = np.random.default_rng(21)
+    R, dim, T, bags, room = 200, 32, 3, 30, 9
+    cfg = bp.make_config(R, 190, dim, "f32", "sgd", lookahead=2, lr=0.1)
+    at = bp.make_attn(2, 2, 16, 0)
+    offs = np.arange(0, bags * room + 1, room, dtype=np.int64)
+    ids, W0 = rng.integers(0, R, T * bags * room), rng.normal(size=(R, dim)).astype(np.float32)
+    given = [(dev(rng.integers(0, room + 1, bags).astype(np.int32)), dev(rng.normal(size=(bags, 2, 16)).astype(np.float32)),
+              dev(rng.normal(size=(bags, 2, 16)).astype(np.float32))) for _ in range(T)]
+    results = []
+    for side in (None, torch.cuda.Stream()):
+        W = dev(W0.copy())
+        tr = CachedEmbeddingTrainer(cfg, W, None)
+        tr.plan(dev(ids), np.arange(T + 1, dtype=np.int64) * bags * room)
+        tr._grad_rows = torch.full((bags * room, dim), float("nan"), device=DEV)
+        kept = []
+        for i, (lens, q, go) in enumerate(given):
+            tr.maintain(i)
+            kw = {}
+            if side is not None:
+                side.wait_stream(torch.cuda.current_stream())
+                kw = dict(stream=side.cuda_stream if handle else side)
+            out, lse = tr.attend(i, at, dev(offs), bags, q, bag_lengths=lens, **kw)
+            gq, _ = tr.attend_backward_update(i, at, dev(offs), bags, q, out, lse, go, bag_lengths=lens, **kw)
+            if side is not None:
+                torch.cuda.current_stream().wait_stream(side)
+                torch.cuda.synchronize()
+            kept += [out, lse, gq]
+        tr.flush()
+        results.append(kept + [W])
+    for a, b in zip(*results):
+        assert torch.isfinite(a[~torch.isinf(a)]).all() and torch.equal(a, b)
