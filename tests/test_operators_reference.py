@@ -185,3 +185,22 @@ def test_refusals_of_eviction():
     refused(-6, bp.bp_evict_by_weight_workspace_bytes, 1 << 31, 2)
     refused(-6, bp.bp_evict_by_weight_workspace_bytes, 4, 1 << 24)
     refused(-1, bp.bp_evict_by_weight_workspace_bytes, -4, 2)
+
+
+def test_workspaces_grow_with_the_call():
+    """A workspace for the largest call serves every smaller one."""
+    sizes, bags = [0, 1, 1023, 4096, 32768, 32769, 524288, 1 << 24], [0, 1, 63, 769, 1100, 2048, 2049, 2561, 1 << 20]
+    rp = bp.make_relpos([1, 2, 4], True)
+    queries = [bp.bp_evict_by_weight_workspace_bytes]
+    for dtype in ("f32", "bf16"):
+        cfg = bp.make_config(1000, 1000, 256, dtype)
+        for at in (bp.make_attn(4, 4, 16, 0), bp.make_attn(8, 2, 32), bp.make_attn(16, 2, 64), bp.make_attn(3, 1, 40)):
+            queries.append(lambda n, b, cfg=cfg, at=at: bp.bp_embbag_attn_fwd_workspace_bytes(cfg, at, n, b, True))
+            queries.append(lambda n, b, cfg=cfg, at=at: bp.bp_embbag_attn_bwd_workspace_bytes(cfg, at, rp, n, b))
+    for query in queries:
+        need = np.array([[query(n, b) for b in bags] for n in sizes])
+        assert (np.diff(need, axis=0) >= 0).all() and (np.diff(need, axis=1) >= 0).all()
+    lengths = [1, 2, 7, 31, 64, 129, 512, 777, 1024, 2048, 4096]
+    for batch, heads in ((1, 1), (1, 5), (3, 5), (2, 16), (8, 64)):
+        need = np.array([[bp.bp_relpos_bias_bwd_workspace_bytes(rp, batch, heads, lq, lk) for lk in lengths] for lq in lengths])
+        assert (np.diff(need, axis=0) >= 0).all() and (np.diff(need, axis=1) >= 0).all()
