@@ -7,7 +7,6 @@
 
 #include "common.h"
 #include "relpos.h"
-#include "row_access.h"
 
 namespace bp {
 
