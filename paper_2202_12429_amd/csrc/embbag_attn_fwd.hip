@@ -618,7 +618,8 @@ __global__ __launch_bounds__(kFwdBlock, sizeof(T) == 4 ? 6 : 5) void embbag_attn
 // a part's fixed cost (the way to its first rows, the meeting of its wavefronts: 8 us in a busy memory) is then paid once and at
 // the same time everywhere, and no CU is left with a part more than another.  (Rows of 1 KB, 64 bags
 // of up to 8,192 entries: 67 us, by pieces 99; all of 4,096: 67 and 71; 1,024 bags of up to 700: 92 and 98.)  Bag b's blocks have the numbers [blocks[b], blocks[b + 1]), an empty bag's
-// one block among them; workgroup w takes those from w * all / groups on.
+// one block among them; workgroup w takes those from w * all / groups on.  Workgroups beyond the number of blocks (lists that use little of
+// their room) take nothing: each of the others has a block, so every one between a bag's first and last owner has written its part.
 constexpr int kBlockShift = 7, kBlock = 1 << kBlockShift, kEvenBags = 2048;
 __device__ __forceinline__ uint32_t bag_blocks(const AttnArgs& a, uint32_t bag) {
     return max(1u, (uint32_t)((bag_span(a, bag).count + kBlock - 1) >> kBlockShift));
@@ -657,8 +658,9 @@ __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2
         all += wave_sums[x];
     }
     all = __builtin_amdgcn_readfirstlane(all);
-    uint32_t at = even_start(blockIdx.x, all, f.groups);
-    const uint32_t end = even_start(blockIdx.x + 1, all, f.groups);
+    const uint32_t groups = min(f.groups, all), share = min(blockIdx.x, groups);
+    uint32_t at = even_start(share, all, groups);
+    const uint32_t end = even_start(min(share + 1, groups), all, groups);
 #pragma unroll
     for (uint32_t i = 0; i < kEvenBags / kFwdBlock; ++i) {
         const uint32_t b = threadIdx.x * per + i;
@@ -699,9 +701,9 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
     // the parts of a bag, and the number of its i-th
     const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
         if (f.groups) {
-            const uint32_t all = f.blocks[a.bags];
-            *first = min(even_owner(f.blocks[bag], all, f.groups), f.groups - 1);
-            return min(even_owner(f.blocks[bag + 1] - 1, all, f.groups), f.groups - 1) - *first + 1;
+            const uint32_t all = f.blocks[a.bags], groups = min(f.groups, all);
+            *first = even_owner(f.blocks[bag], all, groups);
+            return even_owner(f.blocks[bag + 1] - 1, all, groups) - *first + 1;
         }
         const BagPiece p = bag_piece(a, f.shift, bag, 0, bag_span(a, bag), a.bag_off[bag]);
         *first = p.more;
