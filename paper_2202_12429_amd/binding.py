@@ -709,7 +709,11 @@ def _grid(t, dims: int, name: str):
     code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(t.dtype))
     if code is None:
         raise ValueError(f"{name}: float32 or bfloat16 needed, not {t.dtype}")
-    return code, [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims - 1)]
+    strides = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims - 1)]
+    for i, stride in enumerate(strides):
+        if stride == 0 and t.shape[i] > 1:          # 0 is "dense" to the library, which would go on where the array ends
+            raise ValueError(f"{name}: dimension {i} is expanded, not in memory; pass a contiguous() copy")
+    return code, strides
 
 
 def bp_relpos_bias_fwd(rp: bp_relpos, table, q_start: int, out, stream=None) -> None:
@@ -729,7 +733,7 @@ def bp_relpos_bias_bwd_workspace_bytes(rp: bp_relpos, batch: int, heads: int, lq
 
 
 def bp_relpos_bias_bwd(rp: bp_relpos, grad_out, q_start: int, grad_table, workspace, stream=None) -> None:
-    """grad_out: fp32 or bf16 [batch, heads, lq, lk] (strided but for the last dimension); grad_table: fp32 [rows, heads]."""
+    """grad_out: fp32 or bf16 [batch, heads, lq, lk] (strided but for the last dimension, not expanded); grad_table: fp32 [rows, heads]."""
     batch, heads, lq, lk = grad_out.shape
     code, (bs, hs, rs) = _grid(grad_out, 4, "grad_out")
     tp = _needs(grad_table, "float32", relpos_rows(rp) * heads, "grad_table")

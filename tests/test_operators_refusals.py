@@ -1,0 +1,45 @@
+"""Calls of the operators for sequences of cached rows that are refused on the host, before anything is launched."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2202_12429_amd as bp
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """Notes the entry points that are called, and calls none of them."""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append((name, args)) or 0
+
+    import paper_2202_12429_amd.binding as binding
+    monkeypatch.setattr(binding, "load_library", Library)
+    return calls
+
+
+@pytest.mark.parametrize("shape,expanded", [((1, 2, 3, 4), (5, 2, 3, 4)), ((5, 1, 3, 4), (5, 2, 3, 4)), ((5, 2, 1, 4), (5, 2, 3, 4)),
+                                            ((1, 1, 1, 4), (5, 2, 3, 4)), ((5, 2, 3, 1), (5, 2, 3, 4))])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_expanded_arrays_are_not_taken_for_dense_ones(shape, expanded, dtype, library):
+    """What autograd gives for a bias that a batch shares has a stride of 0, which the library reads as "dense"."""
+    rp, g = bp.make_relpos([1, 2]), torch.ones(shape, dtype=dtype).expand(expanded)
+    with pytest.raises(ValueError):
+        bp.bp_relpos_bias_bwd(rp, g, 0, torch.zeros(3, 2), torch.zeros(4096, dtype=torch.uint8), stream=0)
+    if g[0].stride() != g[0].contiguous().stride():
+        with pytest.raises(ValueError):
+            bp.bp_relpos_bias_fwd(rp, torch.zeros(3, 2), 0, g[0], stream=0)
+    assert not library
+
+
+def test_strides_of_sizes_of_one_do_not_matter(library):
+    """An expanded dimension of size 1 is in memory as it is."""
+    rp, g = bp.make_relpos([1, 2]), torch.ones(2, 3, 4)
+    for t in (g.expand(1, 2, 3, 4), g[None].as_strided((1, 2, 3, 4), (0, 12, 4, 1)), g[None, :, :1].as_strided((1, 2, 1, 4), (0, 12, 0, 1))):
+        bp.bp_relpos_bias_bwd(rp, t, 0, torch.zeros(3, 2), torch.zeros(4096, dtype=torch.uint8), stream=0)
+    assert [name for name, _ in library] == ["bp_relpos_bias_bwd"] * 3
+    assert all(args[7:10] == want for (_, args), want in zip(library, [(4, 12, 0), (4, 12, 0), (0, 12, 0)]))
