@@ -164,20 +164,21 @@ __device__ __forceinline__ void find_digit(const uint32_t (&c)[kBins / BLOCK], u
 }
 
 // ---- what stays and what leaves, of one wavefront's stretch ------------------------------------------------------------------
-// Ranks are popcounts of ballots; kAhead steps' loads are in flight together.
+// Ranks are popcounts of ballots; kAhead steps' loads are in flight together.  Places are unsigned here and wherever steps of 64 go past
+// a stretch's end: a list may end at 2^31 - 1.
 constexpr int kAhead = 4;
-__device__ __forceinline__ void move_stretch(const EvictArgs& a, const Part& p, const Choice& c, int begin, int end, uint32_t tie, uint32_t gone) {
+__device__ __forceinline__ void move_stretch(const EvictArgs& a, const Part& p, const Choice& c, uint32_t begin, uint32_t end, uint32_t tie, uint32_t gone) {
     const int lane = threadIdx.x % 64;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     const bool over = p.count > a.budget;
-    const int may0 = a.sinks, may1 = p.count - a.recent;
-    for (int e0 = begin; e0 < end; e0 += 64 * kAhead) {
+    const uint32_t may0 = a.sinks, may1 = over ? p.count - a.recent : 0;
+    for (uint32_t e0 = begin; e0 < end; e0 += 64 * kAhead) {
         float w[kAhead];
         int64_t id[kAhead];
         int32_t slot[kAhead], pos[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int e = e0 + i * 64 + lane;
+            const uint32_t e = e0 + i * 64 + lane;
             const int64_t from = p.first + e;
             if (e >= end) continue;
             w[i] = a.weight[from];
@@ -187,7 +188,7 @@ __device__ __forceinline__ void move_stretch(const EvictArgs& a, const Part& p, 
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int e = e0 + i * 64 + lane;
+            const uint32_t e = e0 + i * 64 + lane;
             const bool in = e < end, may = over && in && e >= may0 && e < may1;
             const uint32_t k = weight_key(w[i]);
             const uint64_t ties = __ballot(may && k == c.key);
@@ -224,12 +225,13 @@ __device__ __forceinline__ void clear_rest(const EvictArgs& a, int64_t all) {
 
 template <int BLOCK>
 struct Stretch {
-    int steps, begin, end;
+    int steps;
+    uint32_t begin, end;
     __device__ __forceinline__ Stretch(const Part& p, int wave) {
         const int places = p.end - p.begin;
         steps = places / BLOCK + (places % BLOCK != 0);
-        begin = p.begin + (int)min((int64_t)places, (int64_t)wave * steps * 64);
-        end = (int)min((int64_t)p.end, (int64_t)begin + steps * 64);
+        begin = p.begin + (uint32_t)min((int64_t)places, (int64_t)wave * steps * 64);
+        end = (uint32_t)min((int64_t)p.end, (int64_t)begin + steps * 64);
     }
 };
 
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(BLOCK) void evict_select_kernel(EvictArgs a) {
     uint32_t key[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        const int e = mine.begin + i * 64 + lane;
+        const uint32_t e = mine.begin + i * 64 + lane;
         key[i] = over && held && e < mine.end ? weight_key(a.weight[p.first + e]) : 0;
     }
     Choice c{0, (uint32_t)over, 0};
@@ -298,15 +300,16 @@ __global__ __launch_bounds__(BLOCK) void evict_select_kernel(EvictArgs a) {
     const int may0 = a.sinks, may1 = p.count - a.recent;
     // f(place, key) for the stretch, 64 places at a time; places past its end come as the list's length
     const auto each = [&](auto&& f) {
+        const uint32_t end = mine.end;
         if (held) {
 #pragma unroll
             for (int i = 0; i < kHeld; ++i)
                 if (i < mine.steps) {
-                    const int e = mine.begin + i * 64 + lane;
-                    f(e < mine.end ? e : p.count, key[i]);
+                    const uint32_t e = mine.begin + i * 64 + lane;
+                    f(e < end ? (int)e : p.count, key[i]);
                 }
         } else {
-            for (int e = mine.begin + lane; e - lane < mine.end; e += 64) f(e < mine.end ? e : p.count, e < mine.end ? weight_key(a.weight[p.first + e]) : 0u);
+            for (uint32_t e = mine.begin + lane; e - lane < end; e += 64) f(e < end ? (int)e : p.count, e < end ? weight_key(a.weight[p.first + e]) : 0u);
         }
     };
     const auto count_digit = [&](int digit) {

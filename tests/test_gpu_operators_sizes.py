@@ -1,0 +1,30 @@
+"""The operators for sequences of cached rows at the largest sizes they accept."""
+import pytest
+import torch
+
+import paper_2202_12429_amd as bp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("lists", [1, 131_100], ids=["by pieces", "whole"])
+def test_eviction_from_a_list_of_all_there_may_be(lists):
+    """A list that ends at 2^31 - 1: its last steps of 64 places go past what 31 bits hold."""
+    n, gone = (1 << 31) - 1, 100
+    off = torch.full((lists + 1,), n, dtype=torch.int64, device=DEV)
+    off[:lists] = 0                                          # the last list holds everything
+    places = torch.cat([torch.arange(0, 50), torch.arange(50) * 7 + n - 350]).tolist()
+    weight = torch.ones(n, device=DEV)
+    weight[torch.tensor(places, device=DEV)] = -torch.arange(1.0, gone + 1, device=DEV)
+    slots = torch.arange(n, dtype=torch.int32, device=DEV)
+    kept = torch.full((n,), 77, dtype=torch.int32, device=DEV)
+    i32 = lambda k: torch.full((k,), 77, dtype=torch.int32, device=DEV)
+    lens, out, ends = i32(lists), i32(gone + 5), torch.full((lists + 1,), 77, dtype=torch.int64, device=DEV)
+    ws = torch.full((bp.bp_evict_by_weight_workspace_bytes(n, lists),), 0xff, dtype=torch.uint8, device=DEV)
+    bp.bp_evict_by_weight(off, None, lists, n - gone, 0, 0, weight, None, slots, None, None, kept, None, None, lens, None, out, ends, ws)
+    assert out.tolist() == places + [-1] * 5
+    assert ends[-1].item() == gone and (ends[:-1] == 0).all() and lens[-1].item() == n - gone and (lens[:-1] == 0).all()
+    for i, (a, e) in enumerate(zip([-1] + places, places + [n])):          # what stays between two that left moves up by i places
+        assert torch.equal(kept[a + 1 - i:e - i], slots[a + 1:e]), i
+    assert (kept[n - gone:] == 77).all()
