@@ -155,24 +155,43 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
             if constexpr (X::BF16) to.set(v);
             else to = f32x4{v[0], v[1], v[2], v[3]};
         };
+        // scores and <grad_out, value>, each entry's against every column
+        const auto product = [&](const uint4& rows, const Frag& with, f32x4& sum) {
+            if constexpr (X::BF16) {
+#pragma unroll
+                for (int part = 2; part >= 0; --part)
+                    sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows), with.part[part], sum, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(rows, i)), with[i], sum, 0, 0, 0);
+            }
+        };
+        // <grad_out, out> of the column: the same products in the same order, out in the place of a value, so that where a bag sees one entry
+        // (whose value out then is, bit for bit) it equals <grad_out, value> and the score has no gradient: not the noise of two roundings,
+        // which a step of Adagrad would blow up.
         Frag qf[KEEP ? X::KM : 1], gf[KEEP ? X::KM : 1];
-        float against = 0.f;                                             // <grad_out, out> of the column
+        f32x4 sa = {0.f, 0.f, 0.f, 0.f};                                 // of heads 4g ... with the column's grad_out
 #pragma unroll
         for (int m = 0; m < X::KM; ++m) {
             float u[X::KC / 4], o[X::KC / 4];
             columns(go, m, u);
             columns(po, m, o);
+            Frag of_out;
+            fragment(gf[KEEP ? m : 0], u);
+            fragment(of_out, o);
+            if constexpr (X::BF16) {
 #pragma unroll
-            for (int i = 0; i < X::KC / 4; ++i) against = fmaf(u[i], o[i], against);
+                for (int part = 2; part >= 0; --part) product(__builtin_bit_cast(uint4, of_out.part[part]), gf[KEEP ? m : 0], sa);
+            } else {
+                product(__builtin_bit_cast(uint4, of_out), gf[KEEP ? m : 0], sa);
+            }
             if constexpr (KEEP) {
                 float v[X::KC / 4];
                 columns(q, m, v);
                 fragment(qf[m], v);
-                fragment(gf[m], u);
             }
         }
-        against += __shfl_xor(against, 16);
-        against += __shfl_xor(against, 32);
+        const float against = __shfl(col % 4 == 0 ? sa[0] : col % 4 == 1 ? sa[1] : col % 4 == 2 ? sa[2] : sa[3], col / 4 * 16 + col);
         const float lse = f.lse[(int64_t)bag * a.q_heads + head];
         const auto element = [&](const float* of, int k, int b, int t) { // 16 * block + col of head k's column 4 * step + g
             const int c = 4 * t + g, x = 16 * b + col;
@@ -268,17 +287,6 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
                 }
             };
             whole_keys();
-            // scores and <grad_out, value>, each entry's against every column
-            const auto product = [&](const uint4& rows, const Frag& with, f32x4& sum) {
-                if constexpr (X::BF16) {
-#pragma unroll
-                    for (int part = 2; part >= 0; --part)
-                        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows), with.part[part], sum, 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(rows, i)), with[i], sum, 0, 0, 0);
-                }
-            };
             float c[X::PER], dp[X::PER];
             if constexpr (KEEP) {
 #pragma unroll
@@ -353,9 +361,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
 #pragma unroll
             for (int e = 0; e < X::PER; ++e) {
                 const bool in = (seen >> (X::PER * g + e) & 1) && z[e] != -INFINITY;      // (a score of -infinity weighs nothing, also in a bag of them alone)
-                // A weight that rounds to 1 has all others below a rounding, and its score no gradient but the two products' difference in
-                // rounding, which a step of Adagrad would blow up (bags of one entry).
-                const float p = in ? exp_few_ulp(z[e] - lse) : 0.f, dz = in && p != 1.f ? p * (dp[e] - against) : 0.f;
+                const float p = in ? exp_few_ulp(z[e] - lse) : 0.f, dz = in ? p * (dp[e] - against) : 0.f;
                 ds[e] = dz * bend[e];
                 turn_ds[(X::PER * g + e) * L::WIDE + col] = ds[e];
                 turn_p[(X::PER * g + e) * L::WIDE + col] = p;
@@ -649,8 +655,8 @@ __global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narr
                     }
                     if (a.bias) z += table[max(row[s], 0) * heads + head];
                     const float dp = N::dot(go, v);
-                    const bool in = row[s] >= 0 && z != -INFINITY;       // (these as in the kernel above)
-                    const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in && p != 1.f ? p * (dp - against) : 0.f, ds = dz * bend;
+                    const bool in = row[s] >= 0 && z != -INFINITY;       // (as in the kernel above; both dots add in the same order)
+                    const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in ? p * (dp - against) : 0.f, ds = dz * bend;
                     if (a.bias && at == 0 && row[s] >= 0) sums[row[s] * heads] += dz;
 #pragma unroll
                     for (int i = 0; i < N::VE; ++i) {
