@@ -168,30 +168,41 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
         };
         // <grad_out, out> of the column: the same products in the same order, out in the place of a value, so that where a bag sees one entry
         // (whose value out then is, bit for bit) it equals <grad_out, value> and the score has no gradient: not the noise of two roundings,
-        // which a step of Adagrad would blow up.
+        // which a step of Adagrad would blow up.  All loads first (2,000 bags of up to 400 rows of 1 KB: 156 us; 161 with every step's products
+        // between its loads and the next one's).
         Frag qf[KEEP ? X::KM : 1], gf[KEEP ? X::KM : 1];
-        f32x4 sa = {0.f, 0.f, 0.f, 0.f};                                 // of heads 4g ... with the column's grad_out
+        float us[X::KM][X::KC / 4], os[X::KM][X::KC / 4], qs[KEEP ? X::KM : 1][X::KC / 4];
 #pragma unroll
         for (int m = 0; m < X::KM; ++m) {
-            float u[X::KC / 4], o[X::KC / 4];
-            columns(go, m, u);
-            columns(po, m, o);
-            Frag of_out;
-            fragment(gf[KEEP ? m : 0], u);
-            fragment(of_out, o);
-            if constexpr (X::BF16) {
+            columns(go, m, us[m]);
+            columns(po, m, os[m]);
+            if constexpr (KEEP) columns(q, m, qs[m]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (KEEP) {
 #pragma unroll
-                for (int part = 2; part >= 0; --part) product(__builtin_bit_cast(uint4, of_out.part[part]), gf[KEEP ? m : 0], sa);
-            } else {
-                product(__builtin_bit_cast(uint4, of_out), gf[KEEP ? m : 0], sa);
-            }
-            if constexpr (KEEP) {
-                float v[X::KC / 4];
-                columns(q, m, v);
-                fragment(qf[m], v);
+            for (int m = 0; m < X::KM; ++m) {
+                fragment(gf[m], us[m]);
+                fragment(qf[m], qs[m]);
             }
         }
-        const float against = __shfl(col % 4 == 0 ? sa[0] : col % 4 == 1 ? sa[1] : col % 4 == 2 ? sa[2] : sa[3], col / 4 * 16 + col);
+        constexpr int SUMS = X::BF16 ? 3 : 1;                            // a part of out each; the leading one's is all of it for a bf16 value
+        f32x4 sa[SUMS];                                                  // of heads 4g ... with the column's grad_out
+#pragma unroll
+        for (int x = 0; x < SUMS; ++x) sa[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int m = 0; m < X::KM; ++m) {
+            Frag of_out;
+            if constexpr (!KEEP) fragment(gf[0], us[m]);
+            fragment(of_out, os[m]);
+#pragma unroll
+            for (int x = 0; x < SUMS; ++x) {
+                if constexpr (X::BF16) product(__builtin_bit_cast(uint4, of_out.part[x]), gf[KEEP ? m : 0], sa[x]);
+                else product(__builtin_bit_cast(uint4, of_out), gf[KEEP ? m : 0], sa[x]);
+            }
+        }
+        if constexpr (X::BF16) sa[0] += sa[1] + sa[2];
+        const float against = __shfl(col % 4 == 0 ? sa[0][0] : col % 4 == 1 ? sa[0][1] : col % 4 == 2 ? sa[0][2] : sa[0][3], col / 4 * 16 + col);
         const float lse = f.lse[(int64_t)bag * a.q_heads + head];
         const auto element = [&](const float* of, int k, int b, int t) { // 16 * block + col of head k's column 4 * step + g
             const int c = 4 * t + g, x = 16 * b + col;
