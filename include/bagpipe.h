@@ -512,6 +512,8 @@ int bp_relpos_update(const bp_config* cfg, const bp_relpos* rp, int32_t heads, f
  * An entry is seen when its slot lies in [0, capacity) and rp, if given, sees its distance.  A bag that sees nothing has
  * out = 0 and lse = -infinity; an entry that is not seen has no part in anything, whatever its row holds.
  * NaN among what is seen goes through to what it has a part in; an infinity there may come out as NaN.
+ * Low values in bias_table mask: next to other scores they weigh nothing; where they swallow the scores of all that a bag sees, all
+ * weigh the same.
  * With lists of one sequence's cached tokens as bags this is the attention of one new token per sequence over its cache.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct bp_attn {
@@ -548,7 +550,8 @@ int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const bp_relpos*
                        const float* weight_in, float* weight_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * The gradients of (6), from its inputs, its out and lse, and grad_out (device, fp32 [bags][q_heads][d]):
+ * The gradients of (6), from its inputs, its out and lse, and grad_out (device, fp32 [bags][q_heads][d]).  p is taken as
+ * exp(c - lse), off by the rounding of lse (|lse| * 2^-24); a bag whose every score is a mask's low value has its sum made again.
  * grad_q      device, fp32 [bags][q_heads][d]
  * grad_rows   device, fp32 [n_lookups][dim]: the gradient of every used entry's row (zeros for entries that are not seen and for
  *             elements that are neither key nor value; entries that no bag uses keep what it holds).  It is what

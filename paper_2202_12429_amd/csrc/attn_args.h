@@ -92,6 +92,8 @@ __device__ __forceinline__ BagPiece find_piece(const AttnArgs& a, int shift, uin
 // exp of a difference: scores stay in natural units up to here, so that the lowest fp32 value, which masks give, does not become
 // an infinity by a change of base.
 __device__ __forceinline__ float exp_few_ulp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+// exp(x) * 2^shift; the same bits as above for a shift of 0
+__device__ __forceinline__ float exp_few_ulp(float x, float shift) { return __builtin_amdgcn_exp2f(fmaf(x, 1.4426950408889634f, shift)); }
 
 // tanh to a few units of the last place: the series up to x^13 where 1 - 2 / (e^2x + 1) cancels.
 __device__ __forceinline__ float tanh_few_ulp(float x) {

@@ -69,6 +69,52 @@ __device__ __forceinline__ void for_own_bags(const BwdArgs& f, uint32_t share, F
         body(bag, s.first + ((int64_t)begin << kUnitShift), (int)min(s.count - ((int64_t)begin << kUnitShift), (int64_t)(stop - begin) << kUnitShift), whole, starts);
     }
 }
+// Where a mask of low values in the bias table covers a whole bag, lse is that value: rounded, it no longer holds the sum of the
+// exponentials, and every weight exp(score - lse) would be 1.  So from kFarLse on, where lse is off by 2^-8 or more, the sum over the bag's
+// entries (a lane's: from, from + step ...) is made again, plainly, and divides the weights; but not where the scores before the bias
+// are no longer small against lse (-infinity then): those have lost more to their own rounding, and add up in another order here.  The
+// arguments are read anew, so that nothing of this stays in registers along the kernel.
+constexpr float kFarLse = 65536.f, kSmall = 64.f;
+__device__ __forceinline__ bool far_lse(float lse) { return fabsf(lse) >= kFarLse && fabsf(lse) < INFINITY; }
+typedef const __attribute__((address_space(4))) AttnArgs* Again;         // the kernels' only argument begins with them
+__device__ __forceinline__ Again arguments_again() {
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return (Again)at;
+}
+template <typename T>
+__device__ __forceinline__ float sum_of_weights(uint32_t bag, int64_t first, int64_t count, int head, int kv_head, float lse, int from, int step,
+                                                const int32_t* borders, const float* column, int columns) {
+    const Again a = arguments_again();
+    const int32_t *const slots = a->slots + first, *const pos = a->lookup_pos + first;
+    const int d = a->d;
+    const float* const q = a->q + ((int64_t)bag * a->q_heads + head) * d;
+    const int64_t q_pos = a->q_pos[bag];
+    float sum = 0.f;
+#pragma unroll 1
+    for (int64_t e = from; e < count; e += step) {
+        const int32_t slot = slots[e];
+        if ((uint32_t)slot >= (uint64_t)a->C) continue;
+        const int row_of = relpos_row(q_pos - pos[e], borders, a->rp.buckets, a->rp.two_sided);
+        if (row_of < 0) continue;
+        const T* const key = (const T*)a->cache_w + (int64_t)slot * a->wst + (int64_t)kv_head * d;
+        float c = 0.f;
+#pragma unroll 1
+        for (int x = 0; x < d; ++x) {
+            float k;
+            if constexpr (sizeof(T) == 4) k = key[x];
+            else k = __uint_as_float((uint32_t)key[x] << 16);
+            c = fmaf(q[x], k, c);
+        }
+        c = a->cap > 0 ? a->cap * tanh_few_ulp(c * (a->scale / a->cap)) : c * a->scale;
+        if (!(fabsf(c) * kSmall < fabsf(lse))) return -INFINITY;
+        c += column[row_of * columns];
+        if (c != -INFINITY) sum += exp_few_ulp(c - lse);
+    }
+    return sum;
+}
+__device__ __forceinline__ float shift_of(float sum) { return sum > 0.f && sum < INFINITY ? -__builtin_amdgcn_logf(sum) : 0.f; }
+
 // Elements of the rows that are neither key nor value.
 __device__ __forceinline__ void clear_rest(const BwdArgs& f, int64_t first, int count) {
     const AttnArgs& a = f.a;
@@ -204,6 +250,14 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
         if constexpr (X::BF16) sa[0] += sa[1] + sa[2];
         const float against = __shfl(col % 4 == 0 ? sa[0][0] : col % 4 == 1 ? sa[0][1] : col % 4 == 2 ? sa[0][2] : sa[0][3], col / 4 * 16 + col);
         const float lse = f.lse[(int64_t)bag * a.q_heads + head];
+        float shift = 0.f;
+        if (a.bias && __any(far_lse(lse))) {
+            const BagSpan span = bag_span(a, bag);
+            float sum = sum_of_weights<T>(bag, span.first, span.count, head, head / group, lse, g, 4, borders, table + min(col, cols - 1), cols);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (far_lse(lse)) shift = shift_of(sum);
+        }
         const auto element = [&](const float* of, int k, int b, int t) { // 16 * block + col of head k's column 4 * step + g
             const int c = 4 * t + g, x = 16 * b + col;
             const int64_t place = ((int64_t)bag * a.q_heads + first_head + (FULL ? k : min(k, heads - 1)) * group + min(c, group - 1)) * d + (FULL ? x : min(x, d - 1));
@@ -372,7 +426,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
 #pragma unroll
             for (int e = 0; e < X::PER; ++e) {
                 const bool in = (seen >> (X::PER * g + e) & 1) && z[e] != -INFINITY;      // (a score of -infinity weighs nothing, also in a bag of them alone)
-                const float p = in ? exp_few_ulp(z[e] - lse) : 0.f, dz = in ? p * (dp[e] - against) : 0.f;
+                const float p = in ? exp_few_ulp(z[e] - lse, shift) : 0.f, dz = in ? p * (dp[e] - against) : 0.f;
                 ds[e] = dz * bend[e];
                 turn_ds[(X::PER * g + e) * L::WIDE + col] = ds[e];
                 turn_p[(X::PER * g + e) * L::WIDE + col] = p;
@@ -626,6 +680,26 @@ __global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narr
         N::read(f.grad_out + place, go);
         N::read(f.out + place, out);
         const float lse = f.lse[(int64_t)bag * heads + head], against = N::dot(go, out);
+        float shift = 0.f;
+        if (a.bias && __any(far_lse(lse))) {                             // (the scores add up as below, so their size does not matter)
+            const Again b = arguments_again();
+            const BagSpan span = bag_span(a, bag);
+            float sum = 0.f;
+#pragma unroll 1
+            for (int64_t e = r; e < span.count; e += side) {
+                const int32_t slot = b->slots[span.first + e];
+                if ((uint32_t)slot >= (uint64_t)b->C) continue;
+                const int row_of = relpos_row((int64_t)b->q_pos[bag] - b->lookup_pos[span.first + e], borders, b->rp.buckets, b->rp.two_sided);
+                if (row_of < 0) continue;
+                float v[N::VE];
+                N::widen(*reinterpret_cast<const uint4*>((const T*)b->cache_w + (int64_t)slot * b->wst + (int64_t)head * d + at), v);
+                float z = N::dot(q, v);
+                z = (b->cap > 0 ? b->cap * tanh_few_ulp(z * (b->scale / b->cap)) : z * b->scale) + table[row_of * heads + head];
+                if (z != -INFINITY) sum += exp_few_ulp(z - lse);
+            }
+            for (int off = width; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+            if (far_lse(lse)) shift = shift_of(sum);
+        }
         const int64_t q_pos = a.bias ? a.q_pos[bag] : 0;
 #pragma unroll
         for (int i = 0; i < N::VE; ++i) dq[i] = 0.f;
@@ -667,7 +741,7 @@ __global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narr
                     if (a.bias) z += table[max(row[s], 0) * heads + head];
                     const float dp = N::dot(go, v);
                     const bool in = row[s] >= 0 && z != -INFINITY;       // (as in the kernel above; both dots add in the same order)
-                    const float p = in ? exp_few_ulp(z - lse) : 0.f, dz = in ? p * (dp - against) : 0.f, ds = dz * bend;
+                    const float p = in ? exp_few_ulp(z - lse, shift) : 0.f, dz = in ? p * (dp - against) : 0.f, ds = dz * bend;
                     if (a.bias && at == 0 && row[s] >= 0) sums[row[s] * heads] += dz;
 #pragma unroll
                     for (int i = 0; i < N::VE; ++i) {

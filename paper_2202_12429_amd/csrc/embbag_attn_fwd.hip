@@ -93,6 +93,7 @@ struct FwdArgs {
     int32_t weighed;            // bags of one piece have their weights from the first launch
     float* scores;              // [q_heads][score_stride]; NULL when no weights are asked for
     int64_t score_stride;
+    float2* norms;              // [bags][q_heads], with the scores: the maximum and one over the sum, 0 where nothing is seen
     float* part_ml;             // [parts][q_heads][2]: maximum and sum of a part of a bag
     float* part_o;              // [parts][q_heads][d]: its weighted values, not divided by the sum
     float* out;
@@ -101,18 +102,20 @@ struct FwdArgs {
     float* weight_out;
 };
 
-// weight_out of a piece's entries, a thread each, from the scores and the bag's norms.  A bag without one (nothing seen) has scores
-// of -infinity alone.
+// weight_out of a piece's entries, a thread each, from the scores and the bag's norms: not from lse, which no longer holds the sum where
+// scores are large (a mask of low values over a whole bag).  A bag without a norm (nothing seen) has scores of -infinity alone.
 template <int BLOCK>
 __device__ __forceinline__ void add_weights(const FwdArgs& f, uint32_t bag, int64_t first, int count) {
-    const float* const lse = f.lse + (int64_t)bag * f.a.q_heads;
+    constexpr int AHEAD = BLOCK == 64 ? 1 : 8;                       // heads whose loads are in flight: wavefronts by themselves have no registers for more
+    const float2* const norms = f.norms + (int64_t)bag * f.a.q_heads;
     for (int i = threadIdx.x % BLOCK; i < count; i += BLOCK) {
         const int64_t k = first + i;
         float add = 0.f;
-#pragma unroll 8
+#pragma unroll AHEAD
         for (int h = 0; h < f.a.q_heads; ++h) {
             const float c = f.scores[h * f.score_stride + k];
-            add += c == -INFINITY ? 0.f : exp_few_ulp(c - lse[h]);
+            const float2 norm = norms[h];
+            add += c == -INFINITY ? 0.f : exp_few_ulp(c - norm.x) * norm.y;
         }
         f.weight_out[k] = (f.weight_in ? f.weight_in[k] : 0.f) + add;
     }
@@ -388,9 +391,10 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
     sum += __shfl_xor(sum, 32);
 
     float* const to = (p.whole ? f.out + ((int64_t)p.bag * a.q_heads + head) * d : f.part_o + ((int64_t)p.part * a.q_heads + head) * d) - own * d;
-    const auto write_norm = [&](float best, float l) {
+    const auto write_norm = [&](float best, float l, float by) {     // by: one over l, 0 for 0
         if (p.whole) {
             f.lse[(int64_t)p.bag * a.q_heads + head] = l == 0.f ? -INFINITY : best + __builtin_amdgcn_logf(l) * kLn2;
+            if (f.scores) f.norms[(int64_t)p.bag * a.q_heads + head] = make_float2(best, by);
         } else {
             f.part_ml[((int64_t)p.part * a.q_heads + head) * 2] = best;
             f.part_ml[((int64_t)p.part * a.q_heads + head) * 2 + 1] = l;
@@ -400,8 +404,8 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
         if (col < cols && at >= own * d && at < (own + 1) * d) __builtin_memcpy(__builtin_assume_aligned(to + at, X::VW >= 4 ? 16 : 4 * X::VW), v, sizeof(v));
     };
     if constexpr (ALONE) {
-        if (g == 0 && col < cols) write_norm(top, sum);
         const float by = !p.whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+        if (g == 0 && col < cols) write_norm(top, sum, by);
 #pragma unroll
         for (int m = 0; m < X::MB; ++m)
 #pragma unroll
@@ -438,12 +442,12 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
         k[x] = exp_few_ulp(ml[x * 32 + col] - (best == -INFINITY ? 0.f : best));
         l = fmaf(k[x], ml[x * 32 + 16 + col], l);
     }
+    const float by = l == 0.f ? 0.f : 1.f / l;
     if (p.whole) {
-        const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int x = 0; x < kFwdWaves; ++x) k[x] = l == 0.f ? 0.f : k[x] * by;
     }
-    if (wave == 0 && g == 0 && col < cols) write_norm(best, l);
+    if (wave == 0 && g == 0 && col < cols) write_norm(best, l, by);
 #pragma unroll
     for (int m = 0; m < X::MB; ++m) {
         float v[X::VW];
@@ -455,7 +459,7 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
         }
         write((m * 16 + 4 * g + wave) * X::VW, v);
     }
-    __syncthreads();                                                 // LDS is free again, the bag's lse there
+    __syncthreads();                                                 // LDS is free again, the bag's norms there
 }
 
 // A workgroup a piece: calls whose bags are short, or so many that they even out.
@@ -606,6 +610,7 @@ __global__ __launch_bounds__(kFwdBlock, sizeof(T) == 4 ? 6 : 5) void embbag_attn
         if (at == 0) {
             if (p.whole) {
                 f.lse[to] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+                if (f.scores) f.norms[to] = make_float2(top, by);
             } else {
                 f.part_ml[to * 2] = top;
                 f.part_ml[to * 2 + 1] = sum;
@@ -761,7 +766,10 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
             const bool none = l == 0.f;
             *reinterpret_cast<float4*>(f.out + (int64_t)bag * width + at) =
                 none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
-            if (at % a.d == 0) f.lse[(int64_t)bag * hq + h] = none ? -INFINITY : top + __builtin_amdgcn_logf(l) * kLn2;
+            if (at % a.d == 0) {
+                f.lse[(int64_t)bag * hq + h] = none ? -INFINITY : top + __builtin_amdgcn_logf(l) * kLn2;
+                if (f.scores) f.norms[(int64_t)bag * hq + h] = make_float2(top, none ? 0.f : 1.f / l);
+            }
         }
         __syncthreads();
     }
@@ -807,12 +815,14 @@ int64_t score_stride(int64_t n) { return ceil_div(n, 64) * 64 + 192; }
 
 struct FwdScratch {
     float *scores, *part_ml, *part_o;
+    float2* norms;
     uint32_t* blocks;
     size_t bytes;
     FwdScratch(void* ws, const bp_attn* at, int64_t n, int64_t bags, bool with_weights) {
         const int64_t parts = FwdPlan::parts(n, bags);
         Carver c(ws, 0);
         scores = c.take<float>(with_weights ? (size_t)score_stride(n) * at->q_heads : 0);
+        norms = c.take<float2>(with_weights ? (size_t)bags * at->q_heads : 0);
         part_ml = c.take<float>((size_t)parts * at->q_heads * 2);
         part_o = c.take<float>((size_t)parts * at->q_heads * at->head_dim);
         blocks = c.take<uint32_t>((size_t)std::min<int64_t>(bags, kEvenBags) + 1);
@@ -882,6 +892,7 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     f.groups = l.even ? l.groups : 0;
     f.blocks = w.blocks;
     f.scores = weights ? w.scores : nullptr;
+    f.norms = w.norms;
     f.score_stride = score_stride(n_lookups);
     f.weighed = l.chunks == 1 && !l.even;
     f.part_ml = w.part_ml;
