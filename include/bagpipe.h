@@ -557,7 +557,8 @@ int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const bp_relpos*
  *             elements that are neither key nor value; entries that no bag uses keep what it holds).  It is what
  *             bp_embbag_bwd_update[_grouped] takes as grad_out with one lookup per bag: rows looked up several times are
  *             coalesced and stepped there.
- * grad_bias   device, fp32 [rows][q_heads], written whole, when rp is given (else NULL)
+ * grad_bias   device, fp32 [rows][q_heads], written whole, when rp is given (else NULL); fp32 sums of at most 4,096 terms, fp64 from
+ *             there on, rounded once
  * Deterministic: the same inputs give the same bits.  Other arguments as above; workspace:
  * bp_embbag_attn_bwd_workspace_bytes().  Asynchronous on `stream`.
  */

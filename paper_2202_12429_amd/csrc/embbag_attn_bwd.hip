@@ -16,6 +16,9 @@ namespace {
 // evenly, wherever bags begin and end.  A bag that is one wavefront's has its grad_q from there; parts of others meet in a launch
 // of their own.
 constexpr int kUnitShift = 5, kUnit = 1 << kUnitShift;
+// A share's gradient of the bias table is summed in fp32, a lane a quarter of the entries (without matrix instructions: of the rows side by
+// side), and in fp64 from there on: up to this many units, 4,096 entries, a share.
+constexpr int kMostUnits = 128;
 constexpr int kBwdWaves = 4, kBwdBlock = kBwdWaves * 64;
 
 struct BwdArgs {
@@ -28,7 +31,7 @@ struct BwdArgs {
     uint32_t units, waves;      // (n >> kUnitShift) + bags; wavefronts that share them
     float* parts;               // [2 * waves][q_heads][d]: grad_q of a bag's part: [2w] of the bag that is under way as wavefront w
                                 // begins, [2w + 1] of the one it begins and does not end
-    float* bias_parts;          // [workgroups][table rows][q_heads]
+    double* bias_parts;         // [workgroups][table rows][q_heads]
 };
 
 __device__ __forceinline__ uint32_t first_unit(const AttnArgs& a, uint32_t bag) {
@@ -644,7 +647,7 @@ __global__ __launch_bounds__(kBwdBlock, bwd_groups_a_cu(sizeof(T), DP, DP * PACK
     for (int e = threadIdx.x; e < table_rows * cols; e += kBwdBlock) {
         double sum = 0;
         for (int x = 0; x < kBwdWaves * 4; ++x) sum += all[(x * table_rows + e / cols) * 16 + e % cols];
-        f.bias_parts[((int64_t)blockIdx.x * table_rows + e / cols) * a.q_heads + first_head + e % cols] = (float)sum;
+        f.bias_parts[((int64_t)blockIdx.x * table_rows + e / cols) * a.q_heads + first_head + e % cols] = sum;
     }
 }
 
@@ -763,7 +766,7 @@ __global__ __launch_bounds__(kBwdBlock, kNarrowGroups) void embbag_attn_bwd_narr
     for (int e = threadIdx.x; e < table_rows * heads; e += kBwdBlock) {
         double sum = 0;
         for (int x = 0; x < kBwdWaves * side; ++x) sum += all_sums[x * table_rows * heads + e];
-        f.bias_parts[(int64_t)blockIdx.x * table_rows * heads + e] = (float)sum;
+        f.bias_parts[(int64_t)blockIdx.x * table_rows * heads + e] = sum;
     }
 }
 
@@ -814,7 +817,7 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_bwd_join_kernel(BwdArg
 
 // grad_bias from the workgroups' parts: 16 elements of the table a workgroup, 64 parts of them side by side
 constexpr int kBiasJoinBlock = 1024;
-__global__ __launch_bounds__(kBiasJoinBlock) void embbag_attn_bias_join_kernel(const float* __restrict__ parts, int count, int groups, float* __restrict__ grad_bias) {
+__global__ __launch_bounds__(kBiasJoinBlock) void embbag_attn_bias_join_kernel(const double* __restrict__ parts, int count, int groups, float* __restrict__ grad_bias) {
     __shared__ double part[kBiasJoinBlock / 16][16];
     const int c = threadIdx.x % 16, e = blockIdx.x * 16 + c, share = threadIdx.x / 16;
     double sum = 0;
@@ -840,18 +843,21 @@ struct BwdPlan {
         pack = attn_pack(at, dp);
         chunks = narrow ? 1 : (at->kv_heads + pack - 1) / pack;
         units = (uint32_t)((n >> kUnitShift) + bags);
-        waves = (uint32_t)std::min<int64_t>(units, std::max(1, 256 * kBwdWaves * (narrow ? kNarrowGroups : bwd_groups_a_cu(elem_bytes(dtype), dp, dp * pack)) / chunks));
-        groups = (waves + kBwdWaves - 1) / kBwdWaves;                    // what the chip holds at once
+        // what the chip holds at once, or shares of kMostUnits
+        const int64_t held = std::max(1, 256 * kBwdWaves * (narrow ? kNarrowGroups : bwd_groups_a_cu(elem_bytes(dtype), dp, dp * pack)) / chunks);
+        waves = (uint32_t)std::min<int64_t>(units, std::max<int64_t>(held, ceil_div(units, kMostUnits)));
+        groups = (waves + kBwdWaves - 1) / kBwdWaves;
     }
 };
 
 struct BwdScratch {
-    float *parts, *bias_parts;
+    float* parts;
+    double* bias_parts;
     size_t bytes;
     BwdScratch(void* ws, const BwdPlan& l, const bp_attn* at, int table_rows) {
         Carver c(ws, 0);
         parts = c.take<float>((size_t)2 * l.waves * at->q_heads * at->head_dim);
-        bias_parts = c.take<float>((size_t)l.groups * table_rows * at->q_heads);
+        bias_parts = c.take<double>((size_t)l.groups * table_rows * at->q_heads);
         bytes = c.used();
     }
 };

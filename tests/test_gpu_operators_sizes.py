@@ -28,3 +28,24 @@ def test_eviction_from_a_list_of_all_there_may_be(lists):
     for i, (a, e) in enumerate(zip([-1] + places, places + [n])):          # what stays between two that left moves up by i places
         assert torch.equal(kept[a + 1 - i:e - i], slots[a + 1:e]), i
     assert (kept[n - gone:] == 77).all()
+
+
+@pytest.mark.parametrize("dim", [8, 16], ids=["matrix instructions", "without"])
+def test_gradient_of_the_bias_over_a_long_list(dim):
+    """All entries of a list of 2^28 in one bucket, with equal terms: the table's gradient is their number times the term, up to fp32
+    sums of 1,024 terms at most (each addition off by half a unit of its sum: 1,024 U of all of it; U for the last rounding)."""
+    n, one = 1 << 28, torch.zeros(1, 1, dim, device=DEV)
+    cfg, at, rp = bp.make_config(4, 4, dim), bp.make_attn(1, 1, dim, 0), bp.make_relpos([])
+    cache, table, lse, go = torch.ones(4, dim, device=DEV), torch.zeros(1, 1, device=DEV), torch.full((1, 1), 1 / 3, device=DEV), torch.full_like(one, 1 / dim)
+    pos, slots, rows = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV), torch.empty(n, dim, device=DEV)
+
+    def gradient(k):
+        gb = torch.empty(1, 1, device=DEV)
+        ws = torch.empty(bp.bp_embbag_attn_bwd_workspace_bytes(cfg, at, rp, k, 1), dtype=torch.uint8, device=DEV)
+        bp.bp_embbag_attn_bwd(cfg, at, cache, slots[:k], torch.tensor([0, k], device=DEV), 1, one, one, lse, go, torch.empty_like(one), rows[:k], gb, ws,
+                              relpos=rp, q_pos=pos[:1], lookup_pos=pos[:k], bias_table=table)
+        return gb.item()
+
+    term = gradient(1)                                       # exp(-1/3)
+    assert abs(term - 0.716531) < 1e-5
+    assert abs(gradient(n) / n - term) <= 1025 * 2.0 ** -24 * term
