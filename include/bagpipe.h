@@ -488,7 +488,7 @@ int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_t heads, i
  * grad_out    device, grad_dtype [batch][heads][lq][lk] with strides as for `out` above (batch_stride likewise, 0 = dense)
  * grad_table  device, fp32 [rows][heads], written whole (rows without a pair get 0)
  * workspace   device, bp_relpos_bias_bwd_workspace_bytes() bytes, 256-byte aligned
- * Limits as above, with batch * heads * lq * lk < 2^40 and batch <= 65,535.  Asynchronous on `stream`.
+ * Limits as above, with batch * heads * lq * lk < 2^40, batch <= 65,535 and lq * (lq + lk) < 2^40.  Asynchronous on `stream`.
  */
 int bp_relpos_bias_bwd_workspace_bytes(const bp_relpos* rp, int64_t batch, int32_t heads, int64_t lq, int64_t lk, size_t* bytes);
 int bp_relpos_bias_bwd(const bp_relpos* rp, const void* grad_out, int32_t grad_dtype, int64_t batch, int32_t heads, int64_t lq,

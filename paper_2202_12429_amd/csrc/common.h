@@ -153,6 +153,13 @@ bool profile_events(int id, hipEvent_t* start, hipEvent_t* stop);
     } while (0)
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A grid of `groups` workgroups of up to 512 threads that may be more than one dimension holds (2^32 threads): along x, then along z.
+// Number blockIdx.z * gridDim.x + blockIdx.x; the last row along z may have numbers from `groups` on.
+inline dim3 spread_grid(int64_t groups, unsigned y) {
+    const int64_t most = int64_t(1) << 22;
+    return groups <= most ? dim3((unsigned)groups, y) : dim3((unsigned)most, y, (unsigned)ceil_div(groups, most));
+}
 inline int bits_for(int64_t n) {   // bits needed to represent values in [0, n)
     int b = 1;
     while (b < 63 && (int64_t(1) << b) < n) ++b;

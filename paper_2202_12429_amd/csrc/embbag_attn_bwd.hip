@@ -777,7 +777,7 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_bwd_join_kernel(BwdArg
     __shared__ float4 part[kJoinBlock];
     const AttnArgs& a = f.a;
     const int width = a.q_heads * a.d, lane = threadIdx.x % 64;
-    const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
+    const int64_t bag0 = (int64_t)(blockIdx.z * gridDim.x + blockIdx.x) * each, mine = bag0 + lane;
     const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
         const uint32_t from = first_unit(a, bag), units = max(1u, (uint32_t)((bag_span(a, bag).count + kUnit - 1) >> kUnitShift));
         *first = share_of(from, f.units, f.waves);
@@ -937,7 +937,7 @@ BP_EXPORT int bp_embbag_attn_bwd(const bp_config* cfg, const bp_attn* at, const 
         if (l.waves > 1) {
             const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
             const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);
-            BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bwd_join_kernel, dim3((unsigned)ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f,
+            BP_LAUNCH(K_ATTN_JOIN, embbag_attn_bwd_join_kernel, spread_grid(ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f,
                       (int)each);
         }
     }

@@ -466,7 +466,8 @@ __device__ __forceinline__ void attend(const FwdArgs& f, const Segment& p, float
 template <typename T, int DP, int PACK, bool FULL>
 __global__ __launch_bounds__(kFwdBlock, DP * PACK > 128 ? 1 : DP * PACK > 64 ? 2 : 3) void embbag_attn_fwd_kernel(FwdArgs f) {
     extern __shared__ float lds[];
-    const uint32_t id = blockIdx.x;
+    const uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
+    if (id >= f.pieces) return;
     const BagPiece p = find_piece(f.a, f.shift, id);
     if (p.number >= p.of) return;
     attend<T, DP, PACK, FULL, false>(f, Segment{p.bag, id, p.first, p.count, p.of == 1}, lds);
@@ -702,7 +703,7 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
     const AttnArgs& a = f.a;
     const int hq = a.q_heads, width = hq * a.d, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int at = blockIdx.y * kShare + threadIdx.x % ACROSS * 4, h = min(at / a.d, hq - 1);
-    const int64_t bag0 = (int64_t)blockIdx.x * each, mine = bag0 + lane;
+    const int64_t bag0 = (int64_t)(blockIdx.z * gridDim.x + blockIdx.x) * each, mine = bag0 + lane;
     // the parts of a bag, and the number of its i-th
     const auto parts_of = [&](uint32_t bag, uint32_t* first) -> uint32_t {
         if (f.groups) {
@@ -779,7 +780,9 @@ __global__ __launch_bounds__(kJoinBlock) void embbag_attn_join_kernel(FwdArgs f,
 // thread.
 constexpr int kWeightShift = 8;
 __global__ __launch_bounds__(kJoinBlock) void embbag_attn_weight_kernel(FwdArgs f) {
-    const BagPiece p = find_piece(f.a, kWeightShift, blockIdx.x);
+    const uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
+    if (id >= (uint64_t)(f.a.n >> kWeightShift) + f.a.bags) return;
+    const BagPiece p = find_piece(f.a, kWeightShift, id);
     if (p.number >= p.of || (f.weighed && bag_piece(f.a, f.shift, p.bag, 0, bag_span(f.a, p.bag), f.a.bag_off[p.bag]).of == 1)) return;
     add_weights<kJoinBlock>(f, p.bag, p.first, p.count);
 }
@@ -845,7 +848,7 @@ struct FwdLaunch {
         else if (l.alone)
             BP_LAUNCH(K_ATTN_FWD, (embbag_attn_short_kernel<T, DP, PACK, FULL>), dim3(std::min(l.resident, (unsigned)ceil_div(f.pieces, kFwdWaves)), (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
         else
-            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK, FULL>), dim3(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
+            BP_LAUNCH(K_ATTN_FWD, (embbag_attn_fwd_kernel<T, DP, PACK, FULL>), spread_grid(f.pieces, (unsigned)l.chunks), dim3(kFwdBlock), shared, stream, f);
         return BP_OK;
     }
     template <typename T, int LANES>
@@ -907,9 +910,9 @@ BP_EXPORT int bp_embbag_attn_fwd(const bp_config* cfg, const bp_attn* at, const 
     if (several) {
         const int64_t shares = ceil_div((int64_t)at->q_heads * at->head_dim, kShare);
         const int64_t each = std::min(std::max<int64_t>(bags * shares / 8192, 1), (int64_t)64);
-        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_join_kernel, dim3((unsigned)ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f, (int)each);
+        BP_LAUNCH(K_ATTN_JOIN, embbag_attn_join_kernel, spread_grid(ceil_div(bags, each), (unsigned)shares), dim3(kJoinBlock), 0, stream, f, (int)each);
     }
     if (weights && (several || !f.weighed))
-        BP_LAUNCH(K_ATTN_WEIGHT, embbag_attn_weight_kernel, dim3((unsigned)piece_count(n_lookups, bags, kWeightShift)), dim3(kJoinBlock), 0, stream, f);
+        BP_LAUNCH(K_ATTN_WEIGHT, embbag_attn_weight_kernel, spread_grid(piece_count(n_lookups, bags, kWeightShift), 1), dim3(kJoinBlock), 0, stream, f);
     return BP_OK;
 }

@@ -70,7 +70,8 @@ __global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, 
     __shared__ int32_t borders[BP_RELPOS_MAX_BUCKETS];
     __shared__ float column[2 * BP_RELPOS_MAX_BUCKETS];
     __shared__ uint32_t line[MOST];                       // fp32: a value a word; bf16: words 0 .. MOST/2 even pairs, then odd ones
-    const int64_t j0 = (int64_t)(blockIdx.x % tiles) * chunks * PER, i0 = (int64_t)(blockIdx.x / tiles) * kBiasRows;
+    const int64_t id = (int64_t)blockIdx.z * gridDim.x + blockIdx.x, j0 = id % tiles * chunks * PER, i0 = id / tiles * kBiasRows;
+    if (i0 >= lq) return;
     const int h = blockIdx.y, rows = (int)min((int64_t)kBiasRows, lq - i0);
     if (threadIdx.x < BP_RELPOS_MAX_BUCKETS) borders[threadIdx.x] = rp.borders[threadIdx.x];
     for (int r = threadIdx.x; r < rp.rows(); r += kBiasBlock) column[r] = table[(int64_t)r * heads + h];
@@ -367,7 +368,7 @@ int grad_plan(const Relpos& r, int32_t dtype, int64_t batch, int32_t heads, int6
     a->steps = 128 / block;
     while (a->steps > 4 && batch * heads * bands * ceil_div(a->blocks_q, a->steps) < kGradEnough) a->steps /= 2;
     const int64_t segments = ceil_div(a->blocks_q, a->steps);
-    if (bands * segments >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
+    if (bands * segments >= (int64_t(1) << 26)) return fail(BP_ERR_UNSUPPORTED, "more than 2^26 pieces of work a head");       // a launch's threads
     a->bands = (int32_t)bands;
     a->segments = (int32_t)segments;
     return BP_OK;
@@ -414,8 +415,7 @@ BP_EXPORT int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_
     const int per = 16 / (int)elem_bytes(out_dtype), chunks = kBiasChunks;         // a workgroup's keys
     const int64_t row_blocks = ceil_div(lq, kBiasRows), all_chunks = ceil_div(lk, per);
     const int64_t tiles = ceil_div(all_chunks, chunks);
-    if (tiles * row_blocks >= (int64_t(1) << 31)) return fail(BP_ERR_UNSUPPORTED, "more than 2^31 pieces of work a head");
-    const dim3 grid((unsigned)(tiles * row_blocks), (unsigned)heads);
+    const dim3 grid = spread_grid(tiles * row_blocks, (unsigned)heads);
     if (out_dtype == BP_F32)
         BP_LAUNCH(K_RELPOS_FWD, relpos_bias_fwd_kernel<float>, grid, dim3(kBiasBlock), 0, (hipStream_t)stream, r, table, heads, lq, lk, q_start,
                   (float*)out, g.row, g.head, chunks, tiles);

@@ -49,3 +49,35 @@ def test_gradient_of_the_bias_over_a_long_list(dim):
     term = gradient(1)                                       # exp(-1/3)
     assert abs(term - 0.716531) < 1e-5
     assert abs(gradient(n) / n - term) <= 1025 * 2.0 ** -24 * term
+
+
+def test_bias_of_more_rows_than_one_dimension_of_a_launch_holds():
+    """A column of 2^30 - 1 queries is 2^25 workgroups of 256 threads."""
+    lq, far = (1 << 30) - 1, 1 << 29
+    rp, table = bp.make_relpos([far]), torch.tensor([[1.0], [2.0]], device=DEV)
+    out = torch.full((1, lq, 1), 7.0, dtype=torch.bfloat16, device=DEV)
+    bp.bp_relpos_bias_fwd(rp, table, 0, out)
+    assert (out[0, :far] == 1).all() and (out[0, far:] == 2).all()
+
+
+def test_attention_over_more_bags_than_one_dimension_of_a_launch_holds():
+    """More than 2^24 bags of 64 entries, with weights: 2^24 and more workgroups of 256 threads in two launches."""
+    bags, each, d = (1 << 24) + 3, 64, 8
+    n = bags * each
+    cfg, at = bp.make_config(1000, 1000, d), bp.make_attn(1, 1, d, 0)
+    cache, q = torch.randn(1000, d, device=DEV), torch.randn(bags, 1, d, device=DEV)
+    slots = (torch.arange(n, dtype=torch.int32, device=DEV) % 997)
+    off = torch.arange(bags + 1, dtype=torch.int64, device=DEV) * each
+    out, lse, w = torch.full_like(q, float("nan")), torch.full((bags, 1), float("nan"), device=DEV), torch.full((n,), float("nan"), device=DEV)
+    ws = torch.full((bp.bp_embbag_attn_fwd_workspace_bytes(cfg, at, n, bags, True),), 0xff, dtype=torch.uint8, device=DEV)
+    bp.bp_embbag_attn_fwd(cfg, at, cache, slots, off, bags, q, out, lse, ws, weight_out=w)
+    for a in (0, bags // 2, 1 << 22, (1 << 23) - 50, 1 << 23, bags - 1000):
+        e = min(a + 1000, bags)
+        k = cache[slots[a * each:e * each].long()].view(-1, each, d).double()
+        c = (k * q[a:e].double()).sum(2) * at.scale
+        p = c.softmax(1)
+        # scores of about 10 terms, sums of 64: a hundred roundings of values below 10 at most
+        assert (out[a:e, 0].double() - (p[..., None] * k).sum(1)).abs().max() <= 100 * 10 * 2.0 ** -24
+        assert (lse[a:e, 0].double() - c.logsumexp(1)).abs().max() <= 100 * 10 * 2.0 ** -24
+        assert (w[a * each:e * each].double().view(-1, each) - p).abs().max() <= 100 * 10 * 2.0 ** -24
+    assert not out.isnan().any() and not lse.isnan().any() and not w.isnan().any()

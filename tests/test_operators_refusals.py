@@ -43,3 +43,18 @@ def test_strides_of_sizes_of_one_do_not_matter(library):
         bp.bp_relpos_bias_bwd(rp, t, 0, torch.zeros(3, 2), torch.zeros(4096, dtype=torch.uint8), stream=0)
     assert [name for name, _ in library] == ["bp_relpos_bias_bwd"] * 3
     assert all(args[7:10] == want for (_, args), want in zip(library, [(4, 12, 0), (4, 12, 0), (0, 12, 0)]))
+
+
+def status(call, *args):
+    with pytest.raises(bp.BagpipeError) as e:
+        call(*args)
+    return e.value.status
+
+
+def test_bias_gradients_of_more_work_than_a_launch_holds():
+    rp = bp.make_relpos([1, 2], True)
+    size = bp.bp_relpos_bias_bwd_workspace_bytes
+    for lq, lk in ((1 << 20, 1), ((1 << 20) - 1, 1), (1 << 18, 3 << 20), (1, (1 << 30) - 1), (1 << 10, (1 << 30) - (1 << 10))):
+        assert size(rp, 1, 1, lq, lk) > 0                                   # lq * (lq + lk) up to 2^40
+    for lq, lk in ((1 << 21, 1), ((1 << 30) - 1, 1), (1 << 21, 1 << 19)):
+        assert status(size, rp, 1, 1, lq, lk) == -6
