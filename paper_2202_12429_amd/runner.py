@@ -98,18 +98,27 @@ class CachedEmbeddingTrainer:
         if max_lookups:
             self._reserve(max_lookups, max_bags or max_lookups)
 
-    def _reserve(self, n: int, bags: int):
+    # What a call allocates, or fills first, it does on the stream that it runs on.
+    @staticmethod
+    def _on(stream):
+        import torch
+        if isinstance(stream, int):            # a handle; 0 is the default stream, which need not be the current one
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        return torch.cuda.stream(stream)
+
+    def _reserve(self, n: int, bags: int, stream=None):
         if (n, bags) in self._sizes_held:      # the buffers only grow: a size that fitted once still fits
             return
         import torch
         need = max(B.bp_embbag_bwd_update_workspace_bytes(self.cfg, n, bags),
                    B.bp_embbag_bwd_update_grouped_workspace_bytes(self.cfg, n, bags, True))
-        if self._bwd_ws is None or self._bwd_ws.numel() < need:
-            self._bwd_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        if self._tickets is None or self._tickets.numel() * 4 < B.bp_embbag_bwd_ticket_bytes(n):
-            self._tickets = B.bwd_tickets(n, device=self.device)
-        if self._out is None or self._out.shape[0] < bags:
-            self._out = torch.empty((bags, int(self.cfg.dim)), dtype=torch.float32, device=self.device)
+        with self._on(stream):
+            if self._bwd_ws is None or self._bwd_ws.numel() < need:
+                self._bwd_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            if self._tickets is None or self._tickets.numel() * 4 < B.bp_embbag_bwd_ticket_bytes(n):
+                self._tickets = B.bwd_tickets(n, device=self.device)
+            if self._out is None or self._out.shape[0] < bags:
+                self._out = torch.empty((bags, int(self.cfg.dim)), dtype=torch.float32, device=self.device)
         if len(self._sizes_held) >= 4096:
             self._sizes_held.clear()
         self._sizes_held.add((n, bags))
@@ -238,7 +247,7 @@ class CachedEmbeddingTrainer:
         when the plan carries no slot map."""
         p = self.plan_
         a, b = self.iter_offsets.item(i), self.iter_offsets.item(i + 1)
-        self._reserve(b - a, bags)
+        self._reserve(b - a, bags, stream)
         out = self._out[:bags] if out is None else out
         if (p.lookup_slots is None) if grouped is None else grouped:
             if bag_offsets_dev is not None:
@@ -255,7 +264,7 @@ class CachedEmbeddingTrainer:
     def backward_update(self, i: int, bag_offsets_dev, bags: int, grad_out, stream=None, grouped: Optional[bool] = None) -> None:
         p = self.plan_
         a, b = self.iter_offsets.item(i), self.iter_offsets.item(i + 1)
-        self._reserve(b - a, bags)
+        self._reserve(b - a, bags, stream)
         use_grouped = (p.grouped_lookups is not None) if grouped is None else grouped
         if use_grouped:
             if b == a:
@@ -270,13 +279,8 @@ class CachedEmbeddingTrainer:
                                    bags, grad_out, self._bwd_ws, self._tickets, stream=stream)
 
     # ---- (6) bags pooled by attention
-    # What these calls allocate belongs to the stream they run on.  Their workspace is the trainer's, as the backward pass's is: one stream at
-    # a time, and a call that is captured into a graph takes its own through the library's functions.
-    @staticmethod
-    def _on(stream):
-        import torch
-        return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) and stream else stream or None)
-
+    # Their workspace is the trainer's, as the backward pass's is: one stream at a time, and a call that is captured into a graph takes its
+    # own through the library's functions.
     def _attn_workspace(self, need: int):
         if self._attn_ws is None or self._attn_ws.numel() < need:
             import torch
