@@ -686,7 +686,11 @@ def _optional(t, dtype: str, n: int, name: str) -> Optional[int]:
 
 def make_relpos(borders, two_sided: bool = False) -> bp_relpos:
     """borders: the smallest distance of buckets 1, 2, ... (bp_relpos_borders makes those in common use)."""
-    b = np.ascontiguousarray(borders, dtype=np.int32)
+    given = np.asarray(borders)
+    with np.errstate(invalid="ignore"):
+        b = np.ascontiguousarray(given, dtype=np.int32)
+    if b.ndim != 1 or not np.array_equal(b, given):
+        raise ValueError("borders: one dimension of whole numbers of 32 bits needed")
     rp = bp_relpos(b.shape[0] + 1, int(bool(two_sided)), b.ctypes.data if b.shape[0] else None)
     rp.kept = b          # the struct holds an address
     return rp

@@ -58,3 +58,11 @@ def test_bias_gradients_of_more_work_than_a_launch_holds():
         assert size(rp, 1, 1, lq, lk) > 0                                   # lq * (lq + lk) up to 2^40
     for lq, lk in ((1 << 21, 1), ((1 << 30) - 1, 1), (1 << 21, 1 << 19)):
         assert status(size, rp, 1, 1, lq, lk) == -6
+
+
+def test_borders_that_32_bits_do_not_hold():
+    for bad in ([1.5, 2.5], np.array([1, (1 << 32) + 5]), [[1, 2], [3, 4]], [float("nan")]):
+        with pytest.raises(ValueError):
+            bp.make_relpos(bad)
+    for good in ([], range(1, 5), (2, 9), np.array([3, 7]), torch.tensor([1, 4]), [1.0, 2.0]):
+        assert bp.relpos_rows(bp.make_relpos(good)) == len(good) + 1
