@@ -340,9 +340,10 @@ int check_grid(int64_t batch, int32_t heads, int64_t lq, int64_t lk, int64_t row
     if (lq && lk && (batch * heads > kBiasMost / lq || batch * heads * lq > kBiasMost / lk))
         return fail(BP_ERR_UNSUPPORTED, "more than 2^40 pairs");
     if (q_start <= -(int64_t(1) << 30) || q_start >= (int64_t(1) << 30)) return fail(BP_ERR_INVALID_ARG, "q_start outside (-2^30, 2^30)");
-    const int64_t row = row_stride ? row_stride : lk, need_head = lq ? (lq - 1) * row + lk : 0;
-    const int64_t most = int64_t(1) << 45;
-    if (row < lk || row > most) return fail(BP_ERR_INVALID_ARG, "row_stride %lld: 0, or at least lk and at most 2^45", (long long)row_stride);
+    const int64_t row = row_stride ? row_stride : lk, most = int64_t(1) << 45;
+    if (row < lk || row > most / std::max<int64_t>(lq, 1))
+        return fail(BP_ERR_INVALID_ARG, "row_stride %lld: 0, or at least lk and at most 2^45 / lq", (long long)row_stride);
+    const int64_t need_head = lq ? (lq - 1) * row + lk : 0;
     const int64_t head = head_stride ? head_stride : lq * row;
     if (head < need_head || head > most)
         return fail(BP_ERR_INVALID_ARG, "head_stride %lld: 0, or at least the span of a head's rows and at most 2^45", (long long)head_stride);

@@ -66,3 +66,12 @@ def test_borders_that_32_bits_do_not_hold():
             bp.make_relpos(bad)
     for good in ([], range(1, 5), (2, 9), np.array([3, 7]), torch.tensor([1, 4]), [1.0, 2.0]):
         assert bp.relpos_rows(bp.make_relpos(good)) == len(good) + 1
+
+
+def test_strides_whose_span_overflows():
+    """A head's span of (lq - 1) * row_stride + lk elements is computed in 64 bits."""
+    rp, lib = bp.make_relpos([1]), bp.load_library()
+    table, out = torch.zeros(2, 2), torch.zeros(2, 1, 5)
+    for lq, row in ((1 << 20, 1 << 44), ((1 << 30) - 1, 1 << 45), (1 << 28, 1 << 36), (2, 1 << 45)):
+        assert lib.bp_relpos_bias_fwd(ctypes.byref(rp), table.data_ptr(), 2, lq, 5, 0, out.data_ptr(), 0, row, 5, None) == -1
+    assert lib.bp_relpos_bias_fwd(ctypes.byref(rp), table.data_ptr(), 2, 0, 5, 0, out.data_ptr(), 0, 1 << 45, 0, None) == 0
