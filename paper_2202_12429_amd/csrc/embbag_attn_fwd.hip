@@ -24,6 +24,8 @@ int attn_check_shape(const bp_config* cfg, const bp_attn* at) {
         return fail(BP_ERR_INVALID_ARG, "keys and values end at element %lld of rows of %d", (long long)(at->value_offset + span), cfg->dim);
     if (!std::isfinite(at->scale)) return fail(BP_ERR_INVALID_ARG, "scale is not finite");
     if (!std::isfinite(at->cap) || at->cap < 0) return fail(BP_ERR_INVALID_ARG, "cap is negative or not finite");
+    // the kernels multiply by it: a score of 0 would be NaN
+    if (at->cap > 0 && !std::isfinite(at->scale / at->cap)) return fail(BP_ERR_INVALID_ARG, "scale / cap is not finite");
     return BP_OK;
 }
 

@@ -75,3 +75,12 @@ def test_strides_whose_span_overflows():
     for lq, row in ((1 << 20, 1 << 44), ((1 << 30) - 1, 1 << 45), (1 << 28, 1 << 36), (2, 1 << 45)):
         assert lib.bp_relpos_bias_fwd(ctypes.byref(rp), table.data_ptr(), 2, lq, 5, 0, out.data_ptr(), 0, row, 5, None) == -1
     assert lib.bp_relpos_bias_fwd(ctypes.byref(rp), table.data_ptr(), 2, 0, 5, 0, out.data_ptr(), 0, 1 << 45, 0, None) == 0
+
+
+def test_a_cap_too_small_for_its_scale():
+    cfg = bp.make_config(100, 100, 64)
+    size = lambda **kw: bp.bp_embbag_attn_fwd_workspace_bytes(cfg, bp.make_attn(2, 1, 16, **kw), 10, 2)
+    for scale, cap in ((1.0, 1e-39), (1e30, 1e-10), (-1e38, 0.1)):
+        assert status(lambda: size(scale=scale, cap=cap)) == -1
+    for scale, cap in ((1.0, 1e-38), (0.0, 1e-39), (1e30, 0.0)):
+        assert size(scale=scale, cap=cap) >= 0
