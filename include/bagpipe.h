@@ -524,7 +524,7 @@ typedef struct bp_attn {
                              a multiple of 8 that is at least kv_heads * d.  cfg->dim holds both; what else a row holds is not
                              read */
     float scale;
-    float cap;            /* 0: none */
+    float cap;            /* 0: none; else scale / cap is finite in fp32 */
 } bp_attn;
 
 /*

@@ -1,7 +1,6 @@
 // Bias by distance: out[h, i, j] = table[row((q_start + i) - j)][h], its gradient and the step on the table.
 #include <algorithm>
 #include <cmath>
-#include <vector>
 
 #include "common.h"
 #include "relpos.h"
@@ -30,27 +29,31 @@ int check_relpos(const bp_relpos* rp, Relpos* out) {
 
 namespace {
 
-// Whole numbers of any size, for comparing products of powers exactly: base 2^32, lowest word first.
-typedef std::vector<uint32_t> Whole;
+// Whole numbers for comparing products of powers exactly: base 2^32, lowest word first.  The products are below n^32 * 32^32 for n up to
+// `far`, 2^24, and a little more: 2^1024 is room enough, and no entry point of C allocates here, which might throw.
+struct Whole {
+    uint32_t word[32] = {1};
+    int size = 1;
+};
 void multiply(Whole& w, uint32_t by) {
     uint64_t carry = 0;
-    for (auto& d : w) {
-        carry += (uint64_t)d * by;
-        d = (uint32_t)carry;
+    for (int i = 0; i < w.size; ++i) {
+        carry += (uint64_t)w.word[i] * by;
+        w.word[i] = (uint32_t)carry;
         carry >>= 32;
     }
-    if (carry) w.push_back((uint32_t)carry);
+    if (carry && w.size < 32) w.word[w.size++] = (uint32_t)carry;
 }
 Whole product(uint32_t a, int times_a, uint32_t b, int times_b) {
-    Whole w{1};
+    Whole w;
     for (int i = 0; i < times_a; ++i) multiply(w, a);
     for (int i = 0; i < times_b; ++i) multiply(w, b);
     return w;
 }
 bool at_least(const Whole& a, const Whole& b) {
-    if (a.size() != b.size()) return a.size() > b.size();
-    for (size_t i = a.size(); i-- > 0;)
-        if (a[i] != b[i]) return a[i] > b[i];
+    if (a.size != b.size) return a.size > b.size;
+    for (int i = a.size; i-- > 0;)
+        if (a.word[i] != b.word[i]) return a.word[i] > b.word[i];
     return true;
 }
 
