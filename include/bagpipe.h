@@ -482,9 +482,9 @@ int bp_relpos_bias_fwd(const bp_relpos* rp, const float* table, int32_t heads, i
 
 /*
  * grad_table[r, h] = sum of grad_out[b, h, i, j] over all b, i, j whose distance has table row r: the bias is broadcast over a
- * batch, so its gradients add up over it.  Deterministic: fp32 sums of short runs of pairs, fp64 from there on, rounded once,
- * in an order that the sizes fix.  Pairs that are not seen are left out, whatever grad_out holds there; what lies
- * between its rows may be read, and is ignored.
+ * batch, so its gradients add up over it.  Deterministic: fp64 sums (bf16 gradients: fp32 over runs of up to 128 pairs, fp64 from
+ * there on), rounded once, in an order that the sizes fix.  Pairs that are not seen are left out, whatever grad_out holds there; what
+ * lies between its rows may be read, and is ignored.
  * grad_out    device, grad_dtype [batch][heads][lq][lk] with strides as for `out` above (batch_stride likewise, 0 = dense)
  * grad_table  device, fp32 [rows][heads], written whole (rows without a pair get 0)
  * workspace   device, bp_relpos_bias_bwd_workspace_bytes() bytes, 256-byte aligned

@@ -1,6 +1,7 @@
 // Bias by distance: out[h, i, j] = table[row((q_start + i) - j)][h], its gradient and the step on the table.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "relpos.h"
@@ -138,6 +139,9 @@ template <typename T>
 struct GradBlock {
     static constexpr int NB = 16 / sizeof(T), STEPS = 128 / NB, DIAGONALS = 64 * NB + 8;      // (the last ones unused)
     typedef uint32_t Vec __attribute__((ext_vector_type(4)));
+    // fp64 from the first addition on for fp32, which costs nothing (2 x 16 grids of 2,048 x 2,048: 115 us, with fp32 runs 123); bf16
+    // values, of eight bits each, in fp32 over a segment's 128 queries, and in fp64 from there on
+    typedef std::conditional_t<sizeof(T) == 4, double, float> Sum;
     Vec raw[NB];
     // The block at `at`, of which `rows` x `cols` pairs exist; `left`: elements from `at` to the end of the array.  A row's 16 bytes
     // are read as long as they lie in the array, and cut after that.
@@ -203,9 +207,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void relpos_bias_bwd_kernel(GradAr
     const bool have = job < jobs;
     const int64_t band0 = a.first_band + job / a.segments * 64, seg0 = job % a.segments * a.steps;
     const int64_t kd = band0 + lane;                                   // the lane's block diagonal
-    float acc[2 * NB - 1];
+    typename B::Sum acc[2 * NB - 1];
 #pragma unroll
-    for (int d = 0; d < 2 * NB - 1; ++d) acc[d] = 0.f;
+    for (int d = 0; d < 2 * NB - 1; ++d) acc[d] = 0;
     if (have) {
         // block rows in which some lane has a block
         const int64_t from = max(seg0, -(band0 + 63)), to = min(min(seg0 + a.steps, a.blocks_q), a.blocks_k - band0);
