@@ -90,7 +90,8 @@ __device__ __forceinline__ BagPiece find_piece(const AttnArgs& a, int shift, uin
 }
 
 // exp of a difference: scores stay in natural units up to here, so that the lowest fp32 value, which masks give, does not become
-// an infinity by a change of base.
+// an infinity by a change of base.  The product with log2(e) is rounded once, so the result is off by up to |x| * 2^-24 of itself: for
+// x = -16, where it is 1e-7, by 1e-6.
 __device__ __forceinline__ float exp_few_ulp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 // exp(x) * 2^shift; the same bits as above for a shift of 0
 __device__ __forceinline__ float exp_few_ulp(float x, float shift) { return __builtin_amdgcn_exp2f(fmaf(x, 1.4426950408889634f, shift)); }

@@ -1,7 +1,9 @@
 // bp_embbag_attn_fwd: bags pooled by attention over their cached rows.
 //
-// One pass over a bag's rows with the running maximum and sum of a softmax.  A bag is cut into pieces of a power of two of
-// entries, a workgroup each; the pieces of a bag of several are joined by a second launch, which also turns scores into weights.
+// One pass over a bag's rows with the running maximum and sum of a softmax, both fp32.  Four layouts, chosen by sizes (FwdPlan): a
+// workgroup a piece of up to 512 entries of a bag; short bags a wavefront a piece; the same without the matrix instructions where a key has
+// one query; and few long bags shared evenly over the chip.  The parts of a bag of several meet in a second launch.  Weights, if asked
+// for, are made of the scores, which are kept: by the workgroup itself where it has all heads of a whole bag, else by a launch of their own.
 #include <algorithm>
 #include <cmath>
 

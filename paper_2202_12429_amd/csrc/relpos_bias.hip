@@ -132,7 +132,8 @@ __global__ __launch_bounds__(kBiasBlock) void relpos_bias_fwd_kernel(Relpos rp, 
 // The gradient's sums run along the diagonals: a wavefront takes 64 blocks of NB x NB pairs side by side, a block a lane (NB
 // keys are 16 bytes), and walks down the diagonal with them, so that a lane adds the same 2 NB - 1 diagonals all the way, in
 // registers, and what is not seen (later keys of a one-sided bias) is a matter of whole diagonals: they are dropped behind the
-// walk, whatever they hold.  Bound by the loads: NB rows of 16 bytes a lane in flight, the next step's under this one's additions.
+// walk, whatever they hold.  Bound by the loads: a step's NB rows of 16 bytes a lane are in flight together, its
+// additions wait for them, and other wavefronts fill the time.
 constexpr int kGradWaves = 4;
 
 template <typename T>
