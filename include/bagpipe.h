@@ -540,7 +540,8 @@ typedef struct bp_attn {
  *              heads of p, for every entry that a bag uses (the others keep what weight_out holds).  weight_in may be NULL (zeros),
  *              or weight_out itself.
  * workspace    device, bp_embbag_attn_fwd_workspace_bytes() bytes, 256-byte aligned (calls that overlap in time need their own)
- * q, out, cache_w, bias_table: 16-byte aligned.  Softmax and sums are fp32; an order that sizes fix.  Asynchronous on `stream`.
+ * q, out, cache_w, bias_table: 16-byte aligned; n_lookups, bags < 2^31.  Softmax and sums are fp32; an order that sizes fix.
+ * Asynchronous on `stream`.
  */
 int bp_embbag_attn_fwd_workspace_bytes(const bp_config* cfg, const bp_attn* at, int64_t n_lookups, int64_t bags, int32_t with_weights,
                                        size_t* bytes);

@@ -81,3 +81,19 @@ def test_attention_over_more_bags_than_one_dimension_of_a_launch_holds():
         assert (lse[a:e, 0].double() - c.logsumexp(1)).abs().max() <= 100 * 10 * 2.0 ** -24
         assert (w[a * each:e * each].double().view(-1, each) - p).abs().max() <= 100 * 10 * 2.0 ** -24
     assert not out.isnan().any() and not lse.isnan().any() and not w.isnan().any()
+
+
+@pytest.mark.parametrize("batch,heads", [(1, 65_535), (65_535, 1), (300, 300)])
+def test_bias_of_the_most_heads_and_batches(batch, heads):
+    rp, lq, lk = bp.make_relpos([1, 2], True), 3, 5
+    table, out = torch.randn(6, heads, device=DEV), torch.empty(heads, lq, lk, device=DEV)
+    bp.bp_relpos_bias_fwd(rp, table, 1, out)
+    distance = 1 + torch.arange(lq, device=DEV)[:, None] - torch.arange(lk, device=DEV)
+    row = torch.where(distance < 0, 3, 0) + distance.abs().clamp(max=2)
+    assert torch.equal(out, table.t()[:, row])
+    g = torch.randint(-8, 9, (batch, heads, lq, lk), device=DEV).float()                 # whole numbers: exact sums
+    got = torch.empty_like(table)
+    ws = torch.full((bp.bp_relpos_bias_bwd_workspace_bytes(rp, batch, heads, lq, lk),), 0xff, dtype=torch.uint8, device=DEV)
+    bp.bp_relpos_bias_bwd(rp, g, 1, got, ws)
+    want = torch.stack([g[:, :, row == r].sum((0, 2)) for r in range(6)])
+    assert torch.equal(got, want)
